@@ -244,6 +244,117 @@ int wisv_ss_decide_static(wisv_ctx *ctx, int32_t batch, int32_t k, int32_t vocab
                           const float *u_accept, const float *u_sample, int32_t *accepted_len, int32_t *emitted_token,
                           float *alpha);
 
+/* --- paged cache ----------------------------------------------------------------------------------
+ * Operators for servers that keep the keys and values of many requests in one pool of pages instead of a ctx's slots:
+ * planning of a step, the append that rotates its queries and keys, and attention of its rows over the pages.  They take
+ * device pointers, only enqueue, and neither read nor write the ctx's stream state, weights or cache: the ctx lends its
+ * device, its stream and its error text.  They allocate nothing and may be captured into a graph.
+ *
+ *   page        `page_size` consecutive positions of one request, a power of two from 16 to 4096.
+ *   pools       K [n_pages][n_kv_heads][page_size][head_dim],
+ *               V [n_pages][n_kv_heads][page_size / 8][head_dim][8]: position and feature (p, d) of a page's head at
+ *               ((p / 8) * head_dim + d) * 8 + p % 8, so that eight positions of a feature lie together.
+ *               page_stride: elements from one page to the next in either pool (0: pages lie close together, n_kv_heads *
+ *               page_size * head_dim), so that a pool may be one layer of a larger one.
+ *   block table [batch][max_pages]: row b names request b's pages in the order of its positions.  An entry outside
+ *               [0, n_pages) is a hole: nothing is read there and its positions are seen by no query.
+ *   slot        page * page_size + position in the page (n_pages * page_size is at most 2^31 - 1).
+ *   head_dim    32, 64, 128 or 256; dtype wisv_dtype of q, k, v, both pools and the output.  Pointers lie on 16 bytes,
+ *               strides are multiples of 16 bytes; the heads of a row lie close together.
+ *   hip_stream  the stream the call enqueues on: NULL is the ctx's, hipStreamLegacy the null stream.
+ * Calls that share no output or workspace may overlap on different streams.
+ */
+
+/* A step's plan from the lengths of its requests.  Request b holds cached_len[b] tokens and brings new_len[b] (negative
+ * counts as 0).  Pages are dealt in request order: the request's new table entries are the next of free_pages.
+ *   q_start   [batch + 1] prefix sums of new_len: the request's rows in the step's packed buffers (at most max_tokens)
+ *   kv_len    [batch] cached_len + new_len; cached_len where the request is refused
+ *   positions [max_tokens] of every row in its request; 0 behind the last row
+ *   slots     [max_tokens] where the row's key and value go; -1 behind the last row, for refused requests and where the
+ *             table has a negative entry
+ *   n_used    [1] entries of free_pages that were dealt
+ *   status    [batch] 0, or why the request is refused (its table row stays as it was): bits 1 free_pages is exhausted,
+ *             2 the table's row is too short, 4 its rows end behind max_tokens */
+#define WISV_PAGED_NO_PAGES 1
+#define WISV_PAGED_ROW_FULL 2
+#define WISV_PAGED_NO_ROWS 4
+typedef struct {
+    int32_t batch;      /* 1..4096 */
+    int32_t page_size;
+    int32_t max_pages;  /* entries of a row of the table; max_pages * page_size at most 2^31 - 1 */
+    int32_t n_free;     /* entries of free_pages; may be 0 */
+    int32_t max_tokens; /* rows of the step's buffers */
+    const int32_t *cached_len, *new_len; /* [batch] */
+    const int32_t *free_pages;           /* [n_free] */
+    int32_t *block_table;                /* [batch][max_pages], updated */
+    int32_t *q_start, *kv_len, *positions, *slots, *n_used, *status;
+    void *hip_stream;
+} wisv_paged_plan_args;
+int wisv_paged_plan(wisv_ctx *ctx, const wisv_paged_plan_args *args);
+
+/* Rotates the queries and keys of n_tokens rows and stores keys and values into their slots: with half = head_dim / 2,
+ * c = cos[position][i], s = sin[position][i], the pair (x_i, x_{i + half}) becomes (x_i c - x_{i + half} s,
+ * x_{i + half} c + x_i s), in float, rounded once.  Rows whose slot lies outside the pool store no key and no value (their
+ * queries are rotated all the same); two rows with one slot leave either.  Positions outside the tables take the nearest
+ * row of them.  q_out may be q (with the same stride). */
+typedef struct {
+    int32_t n_tokens;            /* 0: nothing to do */
+    int32_t n_heads, n_kv_heads; /* n_heads 0: there are no queries (q, q_out NULL) */
+    int32_t head_dim, dtype, page_size, n_pages;
+    int32_t n_rope;              /* rows of the tables */
+    const void *q, *k, *v;       /* rows of n_heads, n_kv_heads, n_kv_heads times head_dim elements */
+    void *q_out;
+    int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from row to row */
+    const int32_t *positions;    /* [n_tokens]; may be NULL when cos is */
+    const int32_t *slots;        /* [n_tokens] */
+    const float *cos, *sin;      /* [n_rope][head_dim / 2], or both NULL: nothing is rotated */
+    void *k_pages, *v_pages;
+    int64_t page_stride;
+    void *hip_stream;
+} wisv_paged_append_args;
+int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
+
+/* Attention of every request's new rows over its pages, which hold the rows' own keys and values already.  Row i of the n
+ * rows of request b has position p = kv_len[b] - n + i and sees key j if j < kv_len[b] and
+ *     j < prefix_len[b],  or  j <= p and (window == 0 or j > p - window).
+ * Its score is x = scale * q.k, then softcap * tanh(x / softcap) if softcap > 0, then x + slopes[head] * (j - p) if slopes
+ * are given; the output is the softmax-weighted sum of the values, and 0 for a row that sees no key.  Query head h reads KV
+ * head h / (n_heads / n_kv_heads).
+ * Keys and values that a row does not see do not reach its output, whatever they hold; a value that it sees and that is
+ * not finite makes that feature of its output infinite or NaN.  Rows of q behind q_start[batch] are
+ * neither read nor written.  kv_len beyond max_pages * page_size leaves the positions behind the table unseen.
+ * max_new and max_len say how many new rows and how long a request is at most (0: unknown).  They choose how the work is
+ * cut; requests beyond them are served all the same, more slowly.
+ * Arithmetic: scores, softmax and sums in float; WISV_BF16 rounds once at the end, and probabilities enter the matrix cores as
+ * one or two bf16 terms.  Equal calls give equal bits.
+ * workspace: at least what wisv_paged_attention_workspace says for the same arguments (it reads no pointer but notes which are NULL);
+ * nothing in it has to be cleared or kept between calls.  Calls that may overlap, and graphs that may be replayed together,
+ * need one each. */
+typedef struct {
+    int32_t batch;    /* 0: nothing to do */
+    int32_t n_tokens; /* rows of q and out */
+    int32_t n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_pages;
+    int32_t max_new, max_len;
+    int32_t window;   /* 0: none */
+    float scale;      /* 0: 1 / sqrt(head_dim) */
+    float softcap;    /* 0: none */
+    const void *q;
+    void *out;
+    int64_t q_stride, out_stride; /* elements from row to row */
+    const void *k_pages, *v_pages;
+    int64_t page_stride;
+    const int32_t *block_table; /* [batch][max_pages] */
+    const int32_t *q_start;     /* [batch + 1], rising */
+    const int32_t *kv_len;      /* [batch] */
+    const int32_t *prefix_len;  /* [batch], or NULL: no prefix */
+    const float *slopes;        /* [n_heads], or NULL: none */
+    void *workspace;            /* on 16 bytes */
+    size_t workspace_bytes;
+    void *hip_stream;
+} wisv_paged_attention_args;
+int wisv_paged_attention_workspace(wisv_ctx *ctx, const wisv_paged_attention_args *args, size_t *bytes);
+int wisv_paged_attention(wisv_ctx *ctx, const wisv_paged_attention_args *args);
+
 /* Frees everything the ctx owns (not the borrowed stream / cache).  NULL is a no-op. */
 int wisv_destroy(wisv_ctx *ctx);
 

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional, Sequence
+from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -28,11 +28,14 @@ WISV_MAX_K = 16
 WISV_OPT_ONE_TERM_CLASSES = 1
 WISV_TERM_QKV, WISV_TERM_O, WISV_TERM_GATE_UP, WISV_TERM_DOWN, WISV_TERM_LM_HEAD = 1, 2, 4, 8, 16
 WISV_TERM_ALL = 31
+WISV_PAGED_NO_PAGES, WISV_PAGED_ROW_FULL, WISV_PAGED_NO_ROWS = 1, 2, 4
+_NULL_STREAM = 1   # hipStreamLegacy: the null stream, where 0 would be the ctx's own
 
 EXPORTS = ("wisv_ctx_create", "wisv_verify_round", "wisv_destroy", "wisv_prefill", "wisv_set_state",
            "wisv_get_state", "wisv_kv_import", "wisv_kv_export", "wisv_debug_copy", "wisv_last_round_ms",
            "wisv_profile_enable", "wisv_profile_collect", "wisv_profile_read", "wisv_calibration_copy", "wisv_last_error",
-           "wisv_ss_verify_round", "wisv_ss_decide", "wisv_ss_decide_static", "wisv_set_option", "wisv_get_option")
+           "wisv_ss_verify_round", "wisv_ss_decide", "wisv_ss_decide_static", "wisv_set_option", "wisv_get_option",
+           "wisv_paged_plan", "wisv_paged_append", "wisv_paged_attention_workspace", "wisv_paged_attention")
 
 
 class WisvError(RuntimeError):
@@ -78,6 +81,39 @@ class wisv_ss_out(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("accepted_len", "correction_token", "alpha")]
 
 
+class wisv_paged_plan_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "page_size", "max_pages", "n_free", "max_tokens")] + \
+               [(n, C.c_void_p) for n in ("cached_len", "new_len", "free_pages", "block_table", "q_start", "kv_len", "positions",
+                                          "slots", "n_used", "status", "hip_stream")]
+
+
+class wisv_paged_append_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_tokens", "n_heads", "n_kv_heads", "head_dim", "dtype", "page_size", "n_pages", "n_rope")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "v", "q_out")] + \
+               [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")] + \
+               [(n, C.c_void_p) for n in ("positions", "slots", "cos", "sin", "k_pages", "v_pages")] + \
+               [("page_stride", C.c_int64), ("hip_stream", C.c_void_p)]
+
+
+class wisv_paged_attention_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_tokens", "n_heads", "n_kv_heads", "head_dim", "dtype", "page_size", "n_pages",
+                                         "max_pages", "max_new", "max_len", "window")] + \
+               [("scale", C.c_float), ("softcap", C.c_float), ("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ("block_table", "q_start", "kv_len", "prefix_len", "slopes", "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("hip_stream", C.c_void_p)]
+
+
+class PagePlan(NamedTuple):
+    """What wisv_paged_plan leaves (int32 device tensors; wisv.h says what they hold)."""
+    q_start: torch.Tensor
+    kv_len: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    n_used: torch.Tensor
+    status: torch.Tensor
+
+
 _lib = None
 
 
@@ -111,6 +147,10 @@ def load_library() -> C.CDLL:
         lib.wisv_ss_decide_static.argtypes = lib.wisv_ss_decide.argtypes
         lib.wisv_set_option.argtypes = [C.c_void_p, C.c_int32, C.c_int64]
         lib.wisv_get_option.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_int64)]
+        lib.wisv_paged_plan.argtypes = [C.c_void_p, C.POINTER(wisv_paged_plan_args)]
+        lib.wisv_paged_append.argtypes = [C.c_void_p, C.POINTER(wisv_paged_append_args)]
+        lib.wisv_paged_attention_workspace.argtypes = [C.c_void_p, C.POINTER(wisv_paged_attention_args), C.POINTER(C.c_size_t)]
+        lib.wisv_paged_attention.argtypes = [C.c_void_p, C.POINTER(wisv_paged_attention_args)]
         lib.wisv_last_error.restype = C.c_char_p
         for name in EXPORTS:
             if name != "wisv_last_error":
@@ -140,6 +180,24 @@ def kv_fill(kv: torch.Tensor, model, layer: int, slot: int, k: torch.Tensor, v: 
     vp = torch.zeros((g, nb * 32, hd), dtype=kv.dtype, device=kv.device)
     vp[:, :n] = v
     kv[layer, slot, 1].view(g, cp // 32, hd, 32)[:, :nb] = vp.view(g, nb, 32, hd).transpose(2, 3)
+
+
+def new_paged_cache(n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype, device):
+    """Zeroed key and value pools of a paged cache: K [n_pages, n_kv_heads, page_size, head_dim],
+    V [n_pages, n_kv_heads, page_size / 8, head_dim, 8]."""
+    return (torch.zeros((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device),
+            torch.zeros((n_pages, n_kv_heads, page_size // 8, head_dim, 8), dtype=dtype, device=device))
+
+
+def paged_fill(k_pages: torch.Tensor, v_pages: torch.Tensor, pages: Sequence[int], k: torch.Tensor, v: torch.Tensor):
+    """Writes k, v ([n_kv_heads, len, head_dim], positions 0..len-1) into the pages of one request, in order."""
+    g, n, hd = k.shape
+    ps = k_pages.shape[2]
+    for i, page in enumerate(pages[:(n + ps - 1) // ps]):
+        m = min(ps, n - i * ps)
+        k_pages[page, :, :m] = k[:, i * ps:i * ps + m]
+        pos = torch.arange(m, device=v_pages.device)
+        v_pages[page][:, pos // 8, :, pos % 8] = v[:, i * ps:i * ps + m].transpose(0, 1).to(v_pages)
 
 
 def make_config(model, max_batch: int, max_ctx: int, max_k: int, device_id: int = 0, hip_stream: int = 0,
@@ -312,6 +370,142 @@ class Context:
     def wisv_ss_decide_static(self, *args, **kw):
         """wisv_ss_decide on the library's static scratch (the entry point that allocates nothing)."""
         return self.wisv_ss_decide(*args, entry="wisv_ss_decide_static", **kw)
+
+    # ---------------------------------------------------------------- paged cache
+    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them.
+    def _stream_now(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream or _NULL_STREAM
+
+    def _ints(self, name: str, t: torch.Tensor, shape) -> int:
+        if t.dtype is not torch.int32 or t.device != self.device or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on {self.device}")
+        return t.data_ptr()
+
+    def _floats(self, name: str, t: torch.Tensor, shape) -> int:
+        if t.dtype is not torch.float32 or t.device != self.device or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on {self.device}")
+        return t.data_ptr()
+
+    def _rows(self, name: str, t: torch.Tensor, dtype, rows: int, head_dim: int):
+        """(pointer, heads, row stride) of packed rows [rows, heads, head_dim]; rows may lie apart, heads may not."""
+        if t.dim() != 3 or t.dtype is not dtype or t.device != self.device or t.shape[0] != rows or t.shape[2] != head_dim:
+            raise ValueError(f"{name} must be [{rows}, heads, {head_dim}] of {dtype} on {self.device}")
+        heads, (s0, s1, s2) = t.shape[1], t.stride()
+        if t.numel() and (s2 != 1 or (heads > 1 and s1 != head_dim)):
+            raise ValueError(f"the heads of a row of {name} must lie close together")
+        return t.data_ptr(), heads, s0 if rows > 1 else heads * head_dim
+
+    def _pools(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
+        """(pages, KV heads, page size, head_dim, wisv_dtype, page stride) of a pair of pools."""
+        dt = k_pages.dtype
+        if dt not in (torch.bfloat16, torch.float32) or v_pages.dtype is not dt or k_pages.device != self.device \
+                or v_pages.device != self.device or k_pages.dim() != 4:
+            raise ValueError(f"the pools must be bfloat16 or float32 tensors on {self.device}, of one type")
+        n, g, ps, hd = k_pages.shape
+        if ps % 8 or v_pages.shape != (n, g, ps // 8, hd, 8):
+            raise ValueError("the pools must be [pages, kv heads, page size, head_dim] and [pages, kv heads, page size / 8, head_dim, 8]")
+        stride = k_pages.stride(0) if n > 1 else g * ps * hd
+        if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+            close = (v_pages.stride(0) if n > 1 else stride) == stride and k_pages[:1].is_contiguous() and v_pages[:1].is_contiguous()
+            if not close:
+                raise ValueError("a page must lie in one piece, and both pools must have the same distance from page to page")
+        return n, g, ps, hd, WISV_BF16 if dt is torch.bfloat16 else WISV_F32, stride
+
+    def wisv_paged_plan(self, cached_len: torch.Tensor, new_len: torch.Tensor, free_pages: torch.Tensor,
+                        block_table: torch.Tensor, page_size: int, max_tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
+        """Plans a step: cached_len, new_len int32 [batch], free_pages int32 [n_free], block_table int32 [batch, max_pages]
+        (updated in place).  `out`: the tensors of an earlier plan of the same sizes, to be written again."""
+        b = cached_len.numel()
+        if out is None:
+            if max_tokens < 1:
+                raise ValueError("max_tokens must be positive")
+            sizes = (b + 1, b, max_tokens, max_tokens, 1, b)
+            out = PagePlan(*torch.empty(sum(sizes), dtype=torch.int32, device=self.device).split(sizes))
+            ptrs = [t.data_ptr() for t in out]
+        else:
+            ptrs = [self._ints(n, t, (m,)) for n, t, m in zip(PagePlan._fields, out, (b + 1, b, max_tokens, max_tokens, 1, b))]
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [batch, max_pages]")
+        width, n_free = block_table.shape[1], free_pages.numel()
+        args = wisv_paged_plan_args(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, (b,)),
+                                    self._ints("new_len", new_len, (b,)), self._ints("free_pages", free_pages, (n_free,)) or None,
+                                    self._ints("block_table", block_table, (b, width)), *ptrs, self._stream_now())
+        self._check(self._lib.wisv_paged_plan(self._h, C.byref(args)))
+        return out
+
+    def wisv_paged_append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
+                          slots: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, cos: Optional[torch.Tensor] = None,
+                          sin: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
+        """Rotates the rows' queries and keys (float32 tables cos, sin [n_rope, head_dim / 2]; None: they stay as they are) and
+        stores keys and values into their slots.  q [tokens, heads, head_dim] or None, k, v [tokens, kv heads, head_dim], slices
+        of a packed row included; positions, slots int32 [tokens].  Returns the rotated queries (q_out, which may be q)."""
+        n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)
+        rows, dt = k.shape[0], k_pages.dtype
+        kp, kg, ks = self._rows("k", k, dt, rows, hd)
+        vp, vg, vs = self._rows("v", v, dt, rows, hd)
+        if kg != g or vg != g:
+            raise ValueError(f"k and v must have the pools' {g} heads")
+        qp = qop = None
+        heads = qs = qos = 0
+        if q is not None:
+            qp, heads, qs = self._rows("q", q, dt, rows, hd)
+            if q_out is None:
+                q_out = torch.empty((rows, heads, hd), dtype=dt, device=self.device)
+            qop, oh, qos = self._rows("q_out", q_out, dt, rows, hd)
+            if oh != heads:
+                raise ValueError("q_out must have the heads of q")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if (cos is None) != (sin is None) or (cos is not None and (positions is None or cos.dim() != 2)):
+            raise ValueError("cos and sin come together, [n_rope, head_dim / 2], and need positions")
+        n_rope = 0 if cos is None else cos.shape[0]
+        args = wisv_paged_append_args(
+            rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos,
+            None if positions is None else self._ints("positions", positions, (rows,)), self._ints("slots", slots, (rows,)),
+            None if cos is None else self._floats("cos", cos, (n_rope, hd // 2)),
+            None if sin is None else self._floats("sin", sin, (n_rope, hd // 2)), k_pages.data_ptr(), v_pages.data_ptr(), stride,
+            self._stream_now())
+        self._check(self._lib.wisv_paged_append(self._h, C.byref(args)))
+        return q_out
+
+    def wisv_paged_attention(self, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
+                             q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int = 0, max_len: int = 0, scale: float = 0.0,
+                             softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None,
+                             prefix_len: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the rows q [tokens, heads, head_dim] over the pages; q_start int32 [batch + 1], kv_len int32 [batch],
+        block_table int32 [batch, max_pages], slopes float32 [heads], prefix_len int32 [batch].  max_new, max_len: how many
+        new rows and how many positions a request has at most (0: unknown).  A new `out` is made where none is given: rows
+        behind q_start[batch] are left as they are in either.  workspace: a tensor of at least as many bytes as
+        wisv_paged_attention_workspace asks for, kept by a caller whose calls must not allocate."""
+        n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)
+        rows, dt = q.shape[0], k_pages.dtype
+        qp, heads, qs = self._rows("q", q, dt, rows, hd)
+        if out is None:
+            out = torch.empty((rows, heads, hd), dtype=dt, device=self.device)
+        op, oh, os_ = self._rows("out", out, dt, rows, hd)
+        if oh != heads:
+            raise ValueError("out must have the heads of q")
+        b = kv_len.numel()
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [batch, max_pages]")
+        args = wisv_paged_attention_args(
+            b, rows, heads, g, hd, dtype, ps, n, block_table.shape[1], max_new, max_len, window, scale, softcap, qp, op, qs, os_,
+            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, (b, block_table.shape[1])),
+            self._ints("q_start", q_start, (b + 1,)), self._ints("kv_len", kv_len, (b,)),
+            None if prefix_len is None else self._ints("prefix_len", prefix_len, (b,)),
+            None if slopes is None else self._floats("slopes", slopes, (heads,)), None, 0, self._stream_now())
+        if workspace is None:
+            need = C.c_size_t()
+            self._check(self._lib.wisv_paged_attention_workspace(self._h, C.byref(args), C.byref(need)))
+            if need.value:
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {self.device}")
+        if workspace is not None:
+            args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        self._check(self._lib.wisv_paged_attention(self._h, C.byref(args)))
+        return out
 
     # ---------------------------------------------------------------- state
     def wisv_prefill(self, stream_id: int, tokens):

@@ -1,0 +1,429 @@
+// Attention of a chunk of new tokens over the paged cache.
+//
+// The rows of a request and KV head - its new tokens x the query heads that share the KV head, token by token - are cut
+// into tiles of 16 NQ rows, so that every cached byte meets a whole tile.  One workgroup = (split of the keys, KV head,
+// request); its waves take steps of 32 (bf16) or 16 (float) keys in turn and never meet before the end: keys and values
+// go from the pages straight into matrix operands.
+//   S^T = K Q^T   A operand: keys.  The rows are dealt so that lane group g of 16 lanes ends up with the scores of E
+//                 consecutive keys (8, or 4) of each of 16 queries;
+//   O^T += V^T P^T  those E probabilities are, as they stand, the B operand, and the A operand is one 16-byte load per
+//                 lane and 16 features from the V pool, which keeps eight positions of a feature together.
+// The softmax keeps a running maximum and sum in float; waves are joined in LDS, splits of the keys by k_paged_join.
+// bf16: probabilities enter the matrix cores as two terms p = hi + lo, |p - hi - lo| <= 2^-17 p (what bounds this kernel
+// is memory, the second term is free).  float: 16x16x4 float products throughout.
+#include "paged.h"
+
+namespace wisv {
+
+template <typename T> struct Step;
+template <> struct Step<bf16_t> { static constexpr int KEYS = 32, E = 8; };
+template <> struct Step<float> { static constexpr int KEYS = 16, E = 4; };
+
+__device__ __forceinline__ paged_f4 mfma_bf16(paged_u4 a, paged_u4 b, paged_f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<paged_bf16x8 *>(&a), *reinterpret_cast<paged_bf16x8 *>(&b), c, 0, 0, 0);
+}
+__device__ __forceinline__ paged_f4 mfma_f32(uint32_t a, uint32_t b, paged_f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
+}
+
+// the pages of one step: two runs of KEYS / 2 keys (a page holds at least 16), each in its page or in a hole of the table
+struct StepPages {
+    int64_t at[2];   // elements from the pool's start to the run, in either pool
+    bool has[2];
+};
+template <typename T, int HD>
+__device__ __forceinline__ StepPages step_pages(const PagedAttn &a, const int32_t *row, int g, int step) {
+    constexpr int KEYS = Step<T>::KEYS;
+    const int key = step * KEYS, p0 = key >> a.page_shift;
+    StepPages s;
+    const int id0 = row[p0], in = key & ((1 << a.page_shift) - 1);
+    const bool ok0 = (unsigned)id0 < (unsigned)a.n_pages;
+    s.has[0] = ok0;
+    s.at[0] = (int64_t)(ok0 ? id0 : 0) * a.page_stride + (((int64_t)g << a.page_shift) + in) * HD;
+    s.has[1] = ok0;
+    s.at[1] = s.at[0] + KEYS / 2 * HD;
+    if (KEYS > 16 && a.page_shift == 4) {
+        const int id1 = row[min(p0 + 1, a.max_pages - 1)];
+        const bool ok1 = (unsigned)id1 < (unsigned)a.n_pages;
+        s.has[1] = ok1;
+        s.at[1] = (int64_t)(ok1 ? id1 : 0) * a.page_stride + ((int64_t)g << a.page_shift) * HD;
+    }
+    return s;
+}
+
+// A float that is no number or infinite has all exponent bits set
+template <typename T> __device__ __forceinline__ bool any_not_finite(uint32_t w) {
+    if (sizeof(T) == 2) return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+    return (w & 0x7f800000u) == 0x7f800000u;
+}
+
+constexpr int merge_tiles(int nw, int nq, int dt) {   // feature tiles of 16 joined at a time: at most 32 KB of LDS
+    int d = dt;
+    while (d > 1 && nw * nq * d > 32) d /= 2;
+    return d;
+}
+
+template <typename T, int HD, int NQ, int NW, bool MODS>
+__global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
+    constexpr int KEYS = Step<T>::KEYS, E = Step<T>::E, KL = HD / 16, QL = HD * (int)sizeof(T) / 64, DT = HD / 16;
+    constexpr int DP = merge_tiles(NW, NQ, DT);
+    constexpr bool BF = sizeof(T) == 2;
+    __shared__ float sm[NW][NQ][16], sl[NW][NQ][16];
+    __shared__ paged_f4 so[NW][NQ][DP][64];
+    const int tid = threadIdx.x, lane = tid & 63, bj = lane & 15, bg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = blockIdx.x % a.G, b = blockIdx.x / a.G, split = blockIdx.y;
+    const PagedRequest rq = paged_request(a, b);
+    const int R = rq.n_new * a.rep;
+    if (a.row_limit && R > a.row_limit) return;
+    const int32_t *table = a.block_table + (int64_t)b * a.max_pages;
+    const T *kpool = (const T *)a.k_pages, *vpool = (const T *)a.v_pages;
+    // this lane's part of a step: keys of its K rows lie in run krun, those of its V operand and scores in run vrun
+    constexpr int HALF = KEYS / 2;
+    const int krow = BF ? 8 * ((bj >> 2) & 1) + (bj & 3) : bj & 7, krun = bj >> 3, vrun = bg >> 1;
+    const int koff = krow * HD + (BF ? 8 : 4) * bg;
+    const int voff = BF ? ((bg & 1) * HD + bj) * 8 : bj * 8 + (bg & 1) * 4;
+
+    for (int rho0 = 0; rho0 < R; rho0 += 16 * NQ) {
+        const int rho_end = min(rho0 + 16 * NQ, R);
+        const int pos_min = rq.pos0 + rho0 / a.rep, pos_max = rq.pos0 + (rho_end - 1) / a.rep;
+        const PagedSteps st = paged_steps(rq, pos_min, pos_max, a.window, KEYS);
+        int s = split * a.split_steps;
+        const int s_end = split == a.n_splits - 1 ? st.total : min(st.total, s + a.split_steps);
+        s += wave;
+
+        // queries: operand (nq, t) of lane (bj, bg) holds 16 bytes of row rho0 + 16 nq + bj
+        paged_u4 q[NQ][QL];
+        int pos[NQ];
+        float slope[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int rho = min(rho0 + 16 * nq + bj, R - 1), tok = rho / a.rep, h = g * a.rep + rho % a.rep;
+            const T *src = (const T *)a.q + (int64_t)(rq.row0 + tok) * a.q_stride + (int64_t)h * HD + (BF ? 8 : 4) * bg;
+#pragma unroll
+            for (int t = 0; t < QL; ++t) q[nq][t] = *reinterpret_cast<const paged_u4 *>(src + t * (BF ? 32 : 16));
+            pos[nq] = rq.pos0 + tok;
+            slope[nq] = MODS && a.slopes ? a.slopes[h] : 0.f;
+        }
+        float m_run[NQ], l_run[NQ];
+        paged_f4 oacc[NQ][DT];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            m_run[nq] = -INFINITY;
+            l_run[nq] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) oacc[nq][dt] = paged_f4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        if (s < s_end) {
+            paged_u4 ka[KL], va[DT];   // bf16: K operands of tile A, then of tile B (four keys further)
+            auto load_k = [&](const StepPages &p) {
+                const T *src = kpool + (krun ? p.at[1] : p.at[0]) + koff;
+                if (BF) {
+#pragma unroll
+                    for (int t = 0; t < KL / 2; ++t) {
+                        ka[t] = *reinterpret_cast<const paged_u4 *>(src + 32 * t);
+                        ka[KL / 2 + t] = *reinterpret_cast<const paged_u4 *>(src + 4 * HD + 32 * t);
+                    }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < KL; ++t) ka[t] = *reinterpret_cast<const paged_u4 *>(src + 16 * t);
+                }
+            };
+            auto load_v = [&](const StepPages &p) {
+                const T *src = vpool + (vrun ? p.at[1] : p.at[0]) + voff;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) va[dt] = *reinterpret_cast<const paged_u4 *>(src + dt * 128);
+            };
+            auto real = [&](int v) { return v < st.n_pre ? v : v + st.skip; };
+            StepPages cur = step_pages<T, HD>(a, table, g, real(s));
+            load_k(cur);
+            load_v(cur);
+            StepPages nxt = step_pages<T, HD>(a, table, g, real(min(s + NW, s_end - 1)));
+            for (; s < s_end; s += NW) {
+                const int step = real(s), key0 = step * KEYS, kbase = key0 + E * bg;   // this lane's keys: kbase .. kbase + E - 1
+                const int n_mine = (vrun ? cur.has[1] : cur.has[0]) ? rq.n_keys : 0;   // keys in a hole of the table are not there
+                // whether every row sees every key of the step (the same for the whole wave)
+                const bool whole = cur.has[0] && cur.has[1] && key0 + KEYS <= rq.n_keys &&
+                                   (key0 + KEYS <= rq.prefix || (key0 + KEYS - 1 <= pos_min && (!a.window || key0 > pos_max - a.window)));
+                paged_u4 phi[NQ], plo[NQ];   // float: phi holds the four probabilities themselves
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) {
+                    paged_f4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+                    if (BF) {
+#pragma unroll
+                        for (int t = 0; t < KL / 2; ++t) {
+                            sa = mfma_bf16(ka[t], q[nq][t], sa);
+                            sb = mfma_bf16(ka[KL / 2 + t], q[nq][t], sb);
+                        }
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < KL; ++t)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (t & 1) sb = mfma_f32(ka[t][j], q[nq][t][j], sb);
+                                else sa = mfma_f32(ka[t][j], q[nq][t][j], sa);
+                            }
+                        sa += sb;
+                    }
+                    float x[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        float v = (e < 4 ? sa[e] : sb[e & 3]) * a.scale;
+                        if (MODS) {
+                            if (a.softcap > 0.f) v = a.softcap * (BF ? paged_tanh_fast(v / a.softcap) : tanhf(v / a.softcap));
+                            if (a.slopes) v = fmaf(slope[nq], (float)(kbase + e - pos[nq]), v);
+                        }
+                        x[e] = v * 1.4426950408889634f;   // in units of ln 2: every exponential is one instruction
+                    }
+                    if (!whole) {
+                        const int lo = a.window ? pos[nq] - a.window : -1;   // (no window: below every key)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const int j = kbase + e;
+                            const bool sees = j < n_mine && (j < rq.prefix || (j <= pos[nq] && j > lo));
+                            x[e] = sees ? x[e] : -INFINITY;
+                        }
+                    }
+                    float mx = x[0];
+#pragma unroll
+                    for (int e = 1; e < E; ++e) mx = fmaxf(mx, x[e]);
+                    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    const float m_new = fmaxf(m_run[nq], mx);
+                    const float m_sub = m_new == -INFINITY ? 0.f : m_new;   // a row that has seen no key yet
+                    const float alpha = __builtin_amdgcn_exp2f(m_run[nq] - m_sub);
+                    float p[E], sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        p[e] = __builtin_amdgcn_exp2f(x[e] - m_sub);
+                        sum += p[e];
+                    }
+                    l_run[nq] = fmaf(l_run[nq], alpha, sum);
+                    m_run[nq] = m_new;
+                    if (__any(alpha != 1.f)) {   // the running maximum rarely moves after a row's first steps
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) oacc[nq][dt] *= alpha;
+                    }
+                    if (BF) {
+#pragma unroll
+                        for (int e = 0; e < E / 2; ++e) {
+                            uint32_t h, l;
+                            split2x2(p[2 * e], p[(2 * e + 1) % E], h, l);
+                            phi[nq][e & 3] = h;
+                            plo[nq][e & 3] = l;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) phi[nq][e] = __float_as_uint(p[e]);
+                    }
+                }
+                load_k(nxt);
+                auto add_v = [&](const paged_u4 &v, int nq, paged_f4 o) {
+                    if (BF) {
+                        o = mfma_bf16(v, phi[nq], o);
+                        return mfma_bf16(v, plo[nq], o);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o = mfma_f32(v[j], phi[nq][j], o);
+                    return o;
+                };
+                bool odd = false;
+                if (!whole) {
+                    // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN
+                    // would reach every row.  The same holds for values that only some rows see.
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t keep;
+                            if (BF) keep = (kbase + 2 * e < n_mine ? 0xffffu : 0u) | (kbase + 2 * e + 1 < n_mine ? 0xffff0000u : 0u);
+                            else keep = kbase + e < n_mine ? 0xffffffffu : 0u;
+                            va[dt][e] &= keep;
+                            odd |= any_not_finite<T>(va[dt][e]);
+                        }
+                    odd = __any(odd);
+                }
+                if (!odd) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) oacc[nq][dt] = add_v(va[dt], nq, oacc[nq][dt]);
+                } else {
+                    // a value that is not finite among keys that some row does not see: one key at a time, added only
+                    // to the rows that see it
+                    for (int k = 0; k < KEYS; ++k) {
+                        const int e = k % E, j = key0 + k;
+                        const bool mine = bg == k / E;
+                        const bool there = (k < HALF ? cur.has[0] : cur.has[1]) && j < rq.n_keys;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            paged_u4 one;
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                if (BF) one[w] = mine && w == e / 2 ? va[dt][w] & (e & 1 ? 0xffff0000u : 0xffffu) : 0u;
+                                else one[w] = mine && w == e ? va[dt][w] : 0u;
+                            }
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq) {
+                                const bool sees = there && (j < rq.prefix || (j <= pos[nq] && (!a.window || j > pos[nq] - a.window)));
+                                const paged_f4 o = add_v(one, nq, oacc[nq][dt]);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) oacc[nq][dt][r] = sees ? o[r] : oacc[nq][dt][r];
+                            }
+                        }
+                    }
+                }
+                load_v(nxt);
+                cur = nxt;
+                nxt = step_pages<T, HD>(a, table, g, real(min(s + 2 * NW, s_end - 1)));
+            }
+        }
+
+        // ---- sums over the four lane groups, then over the waves, in a fixed order
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const float l1 = l_run[nq] + __shfl_xor(l_run[nq], 16, 64);
+            l_run[nq] = l1 + __shfl_xor(l1, 32, 64);
+        }
+        __syncthreads();   // the tile before has been written out
+        if (bg == 0) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                sm[wave][nq][bj] = m_run[nq];
+                sl[wave][nq][bj] = l_run[nq];
+            }
+        }
+        __syncthreads();
+        float m_all[NQ], l_all[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            float mx = -INFINITY, ls = 0.f;
+            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, sm[w][nq][bj]);
+            const float sub = mx == -INFINITY ? 0.f : mx;
+            for (int w = 0; w < NW; ++w) ls = fmaf(sl[w][nq][bj], __builtin_amdgcn_exp2f(sm[w][nq][bj] - sub), ls);
+            m_all[nq] = mx;
+            l_all[nq] = ls;
+            m_run[nq] = __builtin_amdgcn_exp2f(m_run[nq] - sub);   // from here on: the weight of this wave's output
+        }
+#pragma unroll
+        for (int part = 0; part < DT / DP; ++part) {
+            if (part) __syncthreads();
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int dt = 0; dt < DP; ++dt) so[wave][nq][dt][lane] = oacc[nq][part * DP + dt] * m_run[nq];
+            __syncthreads();
+            for (int it = wave; it < DP * NQ; it += NW) {
+                const int dl = it / NQ, nqs = it % NQ, rho = rho0 + 16 * nqs + bj;
+                paged_f4 acc = so[0][nqs][dl][lane];
+                for (int w = 1; w < NW; ++w) acc += so[w][nqs][dl][lane];
+                float m = m_all[0], l = l_all[0];
+#pragma unroll
+                for (int nq = 1; nq < NQ; ++nq)
+                    if (nqs == nq) { m = m_all[nq]; l = l_all[nq]; }
+                if (rho >= R) continue;
+                // this lane holds features d .. d + 3 of the row
+                const int d = 16 * (part * DP + dl) + 4 * bg, h = g * a.rep + rho % a.rep;
+                const int64_t row = rq.row0 + rho / a.rep;
+                if (a.n_splits == 1) {
+                    const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees no key is 0
+                    acc *= inv;
+                    T *dst = (T *)a.out + row * a.out_stride + (int64_t)h * HD + d;
+                    if (BF) *reinterpret_cast<uint2 *>(dst) = make_uint2(f32x2_to_bf16x2(acc[0], acc[1]), f32x2_to_bf16x2(acc[2], acc[3]));
+                    else *reinterpret_cast<paged_f4 *>(dst) = acc;
+                } else {
+                    const int64_t at = ((int64_t)split * a.n_tokens + row) * a.H + h;
+                    if (l != 0.f) *reinterpret_cast<paged_f4 *>(a.po + at * HD + d) = acc;   // (a part without keys is not read)
+                    if (d == 0) {
+                        a.pm[at] = m;
+                        a.pl[at] = l;
+                    }
+                }
+            }
+        }
+    }
+}
+
+// out = sum_s 2^(m_s - m*) o_s / sum_s 2^(m_s - m*) l_s over the splits that saw a key, in split order.  One wave per
+// (row, head): lane s holds the weight of split s, then every lane adds up its features.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
+    constexpr int N = HD >= 128 ? HD / 64 : 1;   // features per lane (HD 32: half of the lanes have none)
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t row = item / a.H;
+    const int h = item % a.H;
+    if (row >= min(a.q_start[a.batch], a.n_tokens)) return;   // rows behind the last request stay as they are
+    const int64_t at = row * a.H + h, step = (int64_t)a.n_tokens * a.H;
+    const bool mine = lane < a.n_splits;
+    const float m = mine ? a.pm[at + lane * step] : -INFINITY, l = mine ? a.pl[at + lane * step] : 0.f;
+    const float top = wave_max(l != 0.f ? m : -INFINITY);
+    const float w = l != 0.f ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+    const float den = wave_sum(w * l);
+    float acc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+    const int d = lane * N;
+    unsigned long long seen = __ballot(l != 0.f);
+    while (seen) {
+        const int s = __ffsll(seen) - 1;
+        seen &= seen - 1;
+        const float ws = __shfl(w, s, 64);
+        if (d < HD) {
+            const float *src = a.po + (at + s * step) * HD + d;
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] = fmaf(ws, src[i], acc[i]);
+        }
+    }
+    if (d >= HD) return;
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    T *dst = (T *)a.out + row * a.out_stride + (int64_t)h * HD + d;
+#pragma unroll
+    for (int i = 0; i < N; ++i) Elem<T>::store(dst + i, acc[i] * inv);
+}
+
+// ------------------------------------------------------------------------------------------ launch
+
+constexpr int NW = 4;
+
+PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len) {
+    const int keys = bf16 ? 32 : 16, steps = (max_len + keys - 1) / keys, wgs = std::max(1, a.batch * a.G);
+    PagedCut c;
+    c.n_splits = std::max(1, std::min(std::min(512 / wgs, (steps + NW - 1) / NW), PAGED_MAX_SPLITS));
+    c.workspace = c.n_splits == 1 ? 0 : (size_t)c.n_splits * a.n_tokens * a.H * (head_dim + 2) * 4;
+    return c;
+}
+
+template <typename T, int HD, int NQ> static void launch_rows(const PagedAttn &a, hipStream_t stream) {
+    const dim3 grid(a.batch * a.G, a.n_splits);
+    if (a.softcap > 0.f || a.slopes) hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, NW, true>), grid, dim3(64 * NW), 0, stream, a);
+    else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, NW, false>), grid, dim3(64 * NW), 0, stream, a);
+}
+template <typename T, int HD> static void launch_attn_t(const PagedAttn &a, int max_new, hipStream_t stream) {
+    if ((int64_t)a.rep * max_new <= 16) launch_rows<T, HD, 1>(a, stream);
+    else launch_rows<T, HD, 2>(a, stream);
+    if (a.n_splits > 1)
+        hipLaunchKernelGGL((k_paged_join<T, HD>), dim3((unsigned)(((int64_t)a.n_tokens * a.H + 3) / 4)), dim3(256), 0, stream, a);
+}
+template <typename T> static void launch_attn_d(const PagedAttn &a, int head_dim, int max_new, hipStream_t stream) {
+    switch (head_dim) {
+        case 32: return launch_attn_t<T, 32>(a, max_new, stream);
+        case 64: return launch_attn_t<T, 64>(a, max_new, stream);
+        case 128: return launch_attn_t<T, 128>(a, max_new, stream);
+        default: return launch_attn_t<T, 256>(a, max_new, stream);
+    }
+}
+
+const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream) {
+    (void)device;
+    a.n_splits = paged_cut(a, bf16, head_dim, max_new, max_len).n_splits;
+    const int keys = bf16 ? 32 : 16, steps = (max_len + keys - 1) / keys;
+    a.split_steps = std::max(1, (steps + a.n_splits - 1) / a.n_splits);
+    a.row_limit = 0;
+    if (bf16) launch_attn_d<bf16_t>(a, head_dim, max_new, stream);
+    else launch_attn_d<float>(a, head_dim, max_new, stream);
+    return nullptr;
+}
+
+}  // namespace wisv

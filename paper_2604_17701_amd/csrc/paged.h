@@ -1,0 +1,96 @@
+// Internal declarations of the paged cache's operators: step planning, the rotating append, attention over the pages.
+#pragma once
+
+#include "wisv_internal.h"
+
+namespace wisv {
+
+struct PagedPlan {
+    int batch, page_shift, max_pages, n_free, max_tokens;
+    const int32_t *cached_len, *new_len, *free_pages;
+    int32_t *block_table, *q_start, *kv_len, *positions, *slots, *n_used, *status;
+};
+constexpr int PLAN_MAX_BATCH = 4096;   // the plan keeps two ints per request in LDS
+void launch_paged_plan(const PagedPlan &a, hipStream_t stream);
+
+struct PagedAppend {
+    int n_tokens, H, G, n_rope, n_pages, page_shift;
+    const void *q, *k, *v;
+    void *q_out, *k_pages, *v_pages;
+    int64_t q_stride, k_stride, v_stride, q_out_stride, page_stride;   // elements
+    const int32_t *positions, *slots;
+    const float *cs, *sn;
+};
+void launch_paged_append(const PagedAppend &a, bool bf16, int head_dim, hipStream_t stream);
+
+struct PagedAttn {
+    int batch, n_tokens, H, G, rep, n_pages, max_pages, page_shift, window;
+    int n_splits, split_steps;     // key steps of a split; the last split takes what is left
+    int row_limit;                 // requests of more rows than this belong to the other kernel of the launch (0: none do)
+    float scale, softcap;
+    const void *q, *k_pages, *v_pages;
+    void *out;
+    int64_t q_stride, out_stride, page_stride;   // elements
+    const int32_t *block_table, *q_start, *kv_len, *prefix_len;
+    const float *slopes;
+    float *po, *pm, *pl;           // n_splits > 1: [split][n_tokens][H][head_dim], [split][n_tokens][H]; pm in units of ln 2
+};
+constexpr int PAGED_MAX_SPLITS = 64;   // the kernel that joins them gives each a lane
+// What a call will launch, from the sizes and the hints alone
+struct PagedCut {
+    int n_splits;
+    size_t workspace;              // bytes
+};
+PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len);
+// null, or why the launch failed
+const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream);
+
+// ------------------------------------------------------------------------------------------ shared device code
+
+typedef __bf16 paged_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float paged_f4 __attribute__((ext_vector_type(4)));
+typedef unsigned int paged_u4 __attribute__((ext_vector_type(4)));
+
+// What a workgroup knows of its request.  Every number is brought into the range the buffers have, whatever the arrays hold.
+struct PagedRequest {
+    int row0;      // first row of q
+    int n_new;     // its rows
+    int pos0;      // position of the first row
+    int n_keys;    // keys the cache can hold for it: positions 0 .. n_keys - 1
+    int prefix;    // positions below it are seen by every row
+};
+__device__ __forceinline__ PagedRequest paged_request(const PagedAttn &a, int b) {
+    PagedRequest r;
+    const int qs = a.q_start[b], qe = a.q_start[b + 1], len = max(a.kv_len[b], 0);
+    const int pre = a.prefix_len ? a.prefix_len[b] : 0;
+    r.row0 = min(max(qs, 0), a.n_tokens);
+    r.n_new = min(max(qe, r.row0), a.n_tokens) - r.row0;
+    r.pos0 = len - r.n_new;
+    r.n_keys = min((int64_t)len, (int64_t)a.max_pages << a.page_shift);
+    r.prefix = min(max(pre, 0), r.n_keys);
+    return r;
+}
+
+// The key steps some row of a tile sees: the prefix's, then from the window of its first row to its last position.
+// Virtual step s is step s of the cache below n_pre and step s + skip from there.
+struct PagedSteps {
+    int n_pre, skip, total;
+};
+__device__ __forceinline__ PagedSteps paged_steps(const PagedRequest &r, int pos_min, int pos_max, int window, int step) {
+    PagedSteps t;
+    t.n_pre = (r.prefix + step - 1) / step;
+    const int lo = window ? max(pos_min - window + 1, 0) : 0;
+    const int first = max(t.n_pre, lo / step);
+    const int last = (min(r.n_keys, max(pos_max + 1, 0)) + step - 1) / step;
+    t.skip = first - t.n_pre;
+    t.total = t.n_pre + max(last - first, 0);
+    return t;
+}
+
+// tanh for scores that end in bf16: an absolute error of about 2^-23
+__device__ __forceinline__ float paged_tanh_fast(float x) {
+    const float e = __builtin_amdgcn_exp2f(x * 2.885390081777927f);   // exp(2 x)
+    return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+}
+
+}  // namespace wisv

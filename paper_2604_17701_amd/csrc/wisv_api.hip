@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <new>
 
+#include "paged.h"
 #include "wisv_internal.h"
 
 using namespace wisv;
@@ -1045,6 +1046,190 @@ extern "C" int wisv_ss_decide_static(wisv_ctx *ctx, int32_t batch, int32_t k, in
                                      int32_t *emitted_token, float *alpha) {
     return ss_decide_common(ctx, true, batch, k, vocab, logits, pending_tokens, draft_tokens, draft_probs, u_accept, u_sample,
                             accepted_len, emitted_token, alpha);
+}
+
+// ------------------------------------------------------------------------------------------ paged cache
+
+// The ctx's device is current inside, the caller's again outside
+struct OnDevice {
+    int before = -1;
+    hipError_t err;
+    explicit OnDevice(int device) {
+        if (hipGetDevice(&before) != hipSuccess) before = -1;
+        err = before == device ? hipSuccess : hipSetDevice(device);
+        if (before == device) before = -1;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+static hipStream_t paged_stream(const Ctx *c, void *s) {
+    return s == nullptr ? c->stream : s == (void *)hipStreamLegacy ? nullptr : (hipStream_t)s;
+}
+static const char *check_page_size(int32_t p) {
+    return p < 16 || p > 4096 || (p & (p - 1)) ? "page_size must be a power of two from 16 to 4096" : nullptr;
+}
+static int log2_of(int32_t p) {
+    int s = 0;
+    while (1 << s < p) ++s;
+    return s;
+}
+static bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// what the append and the attention have in common; sets the page stride when the caller left it at 0
+static const char *check_pools(int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t page_size, int32_t n_pages, const void *k_pages,
+                               const void *v_pages, int64_t *page_stride) {
+    if (n_kv_heads < 1 || n_kv_heads > 4096) return "n_kv_heads outside [1, 4096]";
+    if (head_dim != 32 && head_dim != 64 && head_dim != 128 && head_dim != 256) return "head_dim must be 32, 64, 128 or 256";
+    if (dtype != WISV_F32 && dtype != WISV_BF16) return "dtype must be WISV_F32 or WISV_BF16";
+    if (const char *why = check_page_size(page_size)) return why;
+    if (n_pages < 1 || (int64_t)n_pages * page_size > INT32_MAX) return "n_pages must be positive and n_pages * page_size at most 2^31 - 1";
+    if (!k_pages || !v_pages) return "a pool is NULL";
+    if (!on16(k_pages) || !on16(v_pages)) return "the pools must lie on 16 bytes";
+    const int64_t close = (int64_t)n_kv_heads * page_size * head_dim;
+    if (*page_stride == 0) *page_stride = close;
+    if (*page_stride < close) return "page_stride is smaller than a page";
+    if (*page_stride % 8) return "page_stride must be a multiple of 8 elements";
+    if (*page_stride > INT64_MAX / 8 / n_pages) return "page_stride is too large";
+    return nullptr;
+}
+// a packed buffer of rows; nullptr or what is wrong with it
+static bool rows_ok(const void *p, int64_t stride, int64_t width, int32_t dtype) {
+    return p && on16(p) && stride >= width && stride % (dtype == WISV_BF16 ? 8 : 4) == 0 && stride <= INT64_MAX >> 34;
+}
+
+extern "C" int wisv_paged_plan(wisv_ctx *ctx, const wisv_paged_plan_args *args) {
+    if (!ctx) return WISV_EINVAL;
+    Ctx *c = ctx;
+    if (!args) return fail(c, WISV_EINVAL, "wisv_paged_plan: args is NULL");
+    const wisv_paged_plan_args &p = *args;
+    if (p.batch < 1 || p.batch > PLAN_MAX_BATCH) return fail(c, WISV_EINVAL, "wisv_paged_plan: batch %d outside [1, %d]", p.batch, PLAN_MAX_BATCH);
+    if (const char *why = check_page_size(p.page_size)) return fail(c, WISV_EINVAL, "wisv_paged_plan: %s", why);
+    if (p.max_pages < 1 || (int64_t)p.max_pages * p.page_size > INT32_MAX)
+        return fail(c, WISV_EINVAL, "wisv_paged_plan: max_pages must be positive and max_pages * page_size at most 2^31 - 1");
+    if (p.n_free < 0 || (p.n_free && !p.free_pages)) return fail(c, WISV_EINVAL, "wisv_paged_plan: n_free is negative or free_pages is NULL");
+    if (p.max_tokens < 1) return fail(c, WISV_EINVAL, "wisv_paged_plan: max_tokens %d is not positive", p.max_tokens);
+    if (!p.cached_len || !p.new_len || !p.block_table || !p.q_start || !p.kv_len || !p.positions || !p.slots || !p.n_used || !p.status)
+        return fail(c, WISV_EINVAL, "wisv_paged_plan: a pointer argument is NULL");
+    const OnDevice dev(c->cfg.device_id);
+    HIP_TRY(c, dev.err);
+    const PagedPlan a{p.batch, log2_of(p.page_size), p.max_pages, p.n_free, p.max_tokens, p.cached_len, p.new_len, p.free_pages,
+                      p.block_table, p.q_start, p.kv_len, p.positions, p.slots, p.n_used, p.status};
+    launch_paged_plan(a, paged_stream(c, p.hip_stream));
+    HIP_TRY(c, hipGetLastError());
+    return WISV_OK;
+}
+
+extern "C" int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args) {
+    if (!ctx) return WISV_EINVAL;
+    Ctx *c = ctx;
+    if (!args) return fail(c, WISV_EINVAL, "wisv_paged_append: args is NULL");
+    const wisv_paged_append_args &p = *args;
+    if (p.n_tokens < 0) return fail(c, WISV_EINVAL, "wisv_paged_append: n_tokens %d is negative", p.n_tokens);
+    int64_t page_stride = p.page_stride;
+    if (const char *why = check_pools(p.n_kv_heads, p.head_dim, p.dtype, p.page_size, p.n_pages, p.k_pages, p.v_pages, &page_stride))
+        return fail(c, WISV_EINVAL, "wisv_paged_append: %s", why);
+    if (p.n_heads < 0 || p.n_heads > 1 << 16) return fail(c, WISV_EINVAL, "wisv_paged_append: n_heads %d outside [0, 65536]", p.n_heads);
+    if ((p.cos == nullptr) != (p.sin == nullptr)) return fail(c, WISV_EINVAL, "wisv_paged_append: one of cos and sin is NULL");
+    if (p.cos && (p.n_rope < 1 || !on16(p.cos) || !on16(p.sin)))
+        return fail(c, WISV_EINVAL, "wisv_paged_append: the rotary tables need rows and must lie on 16 bytes");
+    if (p.n_tokens == 0) return WISV_OK;
+    if (!p.slots || (p.cos && !p.positions)) return fail(c, WISV_EINVAL, "wisv_paged_append: a pointer argument is NULL");
+    const int64_t wq = (int64_t)p.n_heads * p.head_dim, wk = (int64_t)p.n_kv_heads * p.head_dim;
+    if ((p.n_heads && (!rows_ok(p.q, p.q_stride, wq, p.dtype) || !rows_ok(p.q_out, p.q_out_stride, wq, p.dtype))) ||
+        !rows_ok(p.k, p.k_stride, wk, p.dtype) || !rows_ok(p.v, p.v_stride, wk, p.dtype))
+        return fail(c, WISV_EINVAL, "wisv_paged_append: q, k, v and q_out must not be NULL, lie on 16 bytes and have row strides that hold "
+                                    "their heads and are multiples of 16 bytes");
+    if (p.q_out == p.q && p.n_heads && p.q_stride != p.q_out_stride)
+        return fail(c, WISV_EINVAL, "wisv_paged_append: q_out is q with another stride");
+    // the grid: a thread per 16-byte piece of four heads
+    if ((int64_t)p.n_tokens * (p.n_heads + p.n_kv_heads + 3) * p.head_dim > (int64_t)1 << 38)
+        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_append: more elements than one launch covers (2^38)");
+    const OnDevice dev(c->cfg.device_id);
+    HIP_TRY(c, dev.err);
+    const PagedAppend a{p.n_tokens, p.n_heads, p.n_kv_heads, p.n_rope, p.n_pages, log2_of(p.page_size), p.q, p.k, p.v, p.q_out, p.k_pages,
+                        p.v_pages, p.q_stride, p.k_stride, p.v_stride, p.q_out_stride, page_stride, p.positions, p.slots, p.cos, p.sin};
+    launch_paged_append(a, p.dtype == WISV_BF16, p.head_dim, paged_stream(c, p.hip_stream));
+    HIP_TRY(c, hipGetLastError());
+    return WISV_OK;
+}
+
+// The checks of a call and of its workspace query; `a` is complete but for the workspace
+static int paged_attention_args(Ctx *c, const wisv_paged_attention_args *args, PagedAttn *a, int *max_new, int *max_len) {
+    if (!args) return fail(c, WISV_EINVAL, "wisv_paged_attention: args is NULL");
+    const wisv_paged_attention_args &p = *args;
+    if (p.batch < 0 || p.batch > 1 << 20 || p.n_tokens < 0)
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: batch %d outside [0, 2^20] or n_tokens %d negative", p.batch, p.n_tokens);
+    int64_t page_stride = p.page_stride;
+    if (const char *why = check_pools(p.n_kv_heads, p.head_dim, p.dtype, p.page_size, p.n_pages, p.k_pages, p.v_pages, &page_stride))
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: %s", why);
+    if (p.n_heads < 1 || p.n_heads > 1 << 16 || p.n_heads % p.n_kv_heads)
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: n_heads must be a multiple of n_kv_heads (and at most 65536)");
+    if (p.max_pages < 1 || (int64_t)p.max_pages * p.page_size > INT32_MAX)
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: max_pages must be positive and max_pages * page_size at most 2^31 - 1");
+    if (p.max_new < 0 || p.max_len < 0 || p.window < 0) return fail(c, WISV_EINVAL, "wisv_paged_attention: max_new, max_len or window is negative");
+    if (!(p.softcap >= 0.f) || !isfinite(p.softcap) || !isfinite(p.scale))
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: softcap must be finite and not negative, scale finite");
+    const int64_t width = (int64_t)p.n_heads * p.head_dim;
+    if (p.batch && p.n_tokens) {
+        if (!rows_ok(p.q, p.q_stride, width, p.dtype) || !rows_ok(p.out, p.out_stride, width, p.dtype))
+            return fail(c, WISV_EINVAL, "wisv_paged_attention: q and out must not be NULL, lie on 16 bytes and have row strides that hold their "
+                                        "heads and are multiples of 16 bytes");
+        if (!p.block_table || !p.q_start || !p.kv_len) return fail(c, WISV_EINVAL, "wisv_paged_attention: block_table, q_start or kv_len is NULL");
+    }
+    if ((int64_t)p.n_tokens * p.n_heads > INT32_MAX / 4 || (int64_t)p.batch * p.n_kv_heads > INT32_MAX / 4)
+        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_attention: more rows than one launch covers (2^29 of rows x heads, or of requests x KV heads)");
+    *a = PagedAttn{};
+    a->batch = p.batch; a->n_tokens = p.n_tokens; a->H = p.n_heads; a->G = p.n_kv_heads; a->rep = p.n_heads / p.n_kv_heads;
+    a->n_pages = p.n_pages; a->max_pages = p.max_pages; a->page_shift = log2_of(p.page_size); a->window = p.window;
+    a->scale = p.scale != 0.f ? p.scale : 1.0f / sqrtf((float)p.head_dim);
+    a->softcap = p.softcap;
+    a->q = p.q; a->k_pages = p.k_pages; a->v_pages = p.v_pages; a->out = p.out;
+    a->q_stride = p.q_stride; a->out_stride = p.out_stride; a->page_stride = page_stride;
+    a->block_table = p.block_table; a->q_start = p.q_start; a->kv_len = p.kv_len; a->prefix_len = p.prefix_len; a->slopes = p.slopes;
+    const int64_t room = (int64_t)p.max_pages * p.page_size;
+    *max_new = p.max_new && p.max_new < p.n_tokens ? p.max_new : p.n_tokens;
+    *max_len = (int)(p.max_len && p.max_len < room ? p.max_len : room);
+    return WISV_OK;
+}
+
+extern "C" int wisv_paged_attention_workspace(wisv_ctx *ctx, const wisv_paged_attention_args *args, size_t *bytes) {
+    if (!ctx) return WISV_EINVAL;
+    Ctx *c = ctx;
+    PagedAttn a;
+    int max_new, max_len;
+    if (const int rc = paged_attention_args(c, args, &a, &max_new, &max_len)) return rc;
+    if (!bytes) return fail(c, WISV_EINVAL, "wisv_paged_attention_workspace: bytes is NULL");
+    *bytes = a.batch && a.n_tokens ? paged_cut(a, args->dtype == WISV_BF16, args->head_dim, max_new, max_len).workspace : 0;
+    return WISV_OK;
+}
+
+extern "C" int wisv_paged_attention(wisv_ctx *ctx, const wisv_paged_attention_args *args) {
+    if (!ctx) return WISV_EINVAL;
+    Ctx *c = ctx;
+    PagedAttn a;
+    int max_new, max_len;
+    if (const int rc = paged_attention_args(c, args, &a, &max_new, &max_len)) return rc;
+    if (a.batch == 0 || a.n_tokens == 0) return WISV_OK;
+    const wisv_paged_attention_args &p = *args;
+    const bool bf16 = p.dtype == WISV_BF16;
+    const PagedCut cut = paged_cut(a, bf16, p.head_dim, max_new, max_len);
+    if (cut.workspace) {
+        if (!p.workspace || p.workspace_bytes < cut.workspace || !on16(p.workspace))
+            return fail(c, WISV_EINVAL, "wisv_paged_attention: the workspace must lie on 16 bytes and hold %zu bytes (%zu given)", cut.workspace,
+                        p.workspace ? p.workspace_bytes : 0);
+        const size_t rows = (size_t)cut.n_splits * a.n_tokens * a.H;
+        a.po = (float *)p.workspace;
+        a.pm = a.po + rows * p.head_dim;
+        a.pl = a.pm + rows;
+    }
+    const OnDevice dev(c->cfg.device_id);
+    HIP_TRY(c, dev.err);
+    if (const char *why = launch_paged_attention(a, bf16, p.head_dim, max_new, max_len, c->cfg.device_id, paged_stream(c, p.hip_stream)))
+        return fail(c, WISV_EHIP, "wisv_paged_attention: %s", why);
+    HIP_TRY(c, hipGetLastError());
+    return WISV_OK;
 }
 
 // ------------------------------------------------------------------------------------------ options

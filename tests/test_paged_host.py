@@ -1,0 +1,175 @@
+"""Host side of the paged cache's operators, on the CPU: libwisv.so runs in a child process on a stand-in for the HIP runtime
+(stub_hip.c: kernels are logged, not run).  Every refusal comes before a launch, with a message; good calls launch what they
+should; the oracle itself is pinned to hand-worked numbers."""
+import subprocess
+import sys
+import textwrap
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as ref
+from paper_2604_17701_amd import binding
+from test_host_failures import PRELUDE, ROOT, stub  # noqa: F401
+
+PAGED = '''
+buf = np.zeros(1 << 16, np.float32)
+P = (buf.ctypes.data + 15) // 16 * 16
+h = create(configs.TINY, 1, 64, 4)
+stub.stub_log_clear()
+
+
+def text():
+    return lib.wisv_last_error(h).decode()
+
+
+def plan(**kw):
+    d = dict(batch=2, page_size=16, max_pages=4, n_free=3, max_tokens=9, cached_len=P, new_len=P, free_pages=P, block_table=P, q_start=P,
+             kv_len=P, positions=P, slots=P, n_used=P, status=P)
+    return lib.wisv_paged_plan(h, C.byref(B.wisv_paged_plan_args(**{**d, **kw})))
+
+
+def append(**kw):
+    d = dict(n_tokens=5, n_heads=4, n_kv_heads=2, head_dim=64, dtype=1, page_size=16, n_pages=3, n_rope=8, q=P, k=P, v=P, q_out=P + 4096,
+             q_stride=256, k_stride=128, v_stride=128, q_out_stride=256, positions=P, slots=P, cos=P, sin=P, k_pages=P, v_pages=P)
+    return lib.wisv_paged_append(h, C.byref(B.wisv_paged_append_args(**{**d, **kw})))
+
+
+def attn_args(**kw):
+    d = dict(batch=2, n_tokens=5, n_heads=4, n_kv_heads=2, head_dim=64, dtype=1, page_size=16, n_pages=3, max_pages=2, q=P, out=P,
+             q_stride=256, out_stride=256, k_pages=P, v_pages=P, block_table=P, q_start=P, kv_len=P)
+    return B.wisv_paged_attention_args(**{**d, **kw})
+
+
+def need(**kw):
+    n = C.c_size_t(77)
+    assert lib.wisv_paged_attention_workspace(h, C.byref(attn_args(**kw)), C.byref(n)) == 0, text()
+    return n.value
+
+
+def attn(**kw):
+    return lib.wisv_paged_attention(h, C.byref(attn_args(**kw)))
+
+'''
+
+
+def run(stub, body):
+    code = f"ROOT, STUB = {ROOT!r}, {stub!r}\n" + PRELUDE + PAGED + textwrap.dedent(body) + "\nprint('done')\n"
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("done"), r.stdout + r.stderr
+
+
+def test_plan_refuses_bad_arguments(stub):
+    run(stub, '''
+        assert plan() == 0 and len(log()) == 1, (text(), log())
+        stub.stub_log_clear()
+        for kw, what in ((dict(batch=0), "batch"), (dict(batch=4097), "batch"), (dict(page_size=8), "page_size"), (dict(page_size=48), "page_size"),
+                         (dict(page_size=8192), "page_size"), (dict(max_pages=0), "max_pages"), (dict(max_pages=1 << 28), "max_pages"), (dict(n_free=-1), "n_free"),
+                         (dict(free_pages=None), "free_pages"), (dict(max_tokens=0), "max_tokens"), (dict(cached_len=None), "NULL"),
+                         (dict(status=None), "NULL"), (dict(slots=None), "NULL")):
+            assert plan(**kw) == B.WISV_EINVAL and what in text(), (kw, text())
+        assert lib.wisv_paged_plan(h, None) == B.WISV_EINVAL and lib.wisv_paged_plan(None, None) == B.WISV_EINVAL
+        assert log() == []
+        assert plan(n_free=0, free_pages=None) == 0
+    ''')
+
+
+def test_append_refuses_bad_arguments(stub):
+    run(stub, '''
+        assert append() == 0 and len(log()) == 1, (text(), log())
+        stub.stub_log_clear()
+        for kw, what in ((dict(n_tokens=-1), "n_tokens"), (dict(head_dim=96), "head_dim"), (dict(dtype=2), "dtype"), (dict(page_size=24), "page_size"),
+                         (dict(n_pages=0), "n_pages"), (dict(n_pages=1 << 28), "n_pages"), (dict(k_pages=None), "pool"), (dict(v_pages=P + 2), "16 bytes"),
+                         (dict(page_stride=100), "page_stride"), (dict(page_stride=2052), "page_stride"), (dict(n_heads=-1), "n_heads"), (dict(cos=None), "cos"),
+                         (dict(n_rope=0), "rotary"), (dict(sin=P + 4), "rotary"), (dict(slots=None), "NULL"), (dict(positions=None), "NULL"),
+                         (dict(q=None), "q, k, v"), (dict(k=None), "q, k, v"), (dict(v=P + 8), "q, k, v"), (dict(q_stride=252), "q, k, v"),
+                         (dict(k_stride=132), "q, k, v"), (dict(v_stride=64), "q, k, v"), (dict(q_out=P, q_out_stride=512), "another stride"),
+                         (dict(n_kv_heads=0), "n_kv_heads")):
+            assert append(**kw) == B.WISV_EINVAL and what in text(), (kw, text())
+        assert append(n_tokens=2**31 - 1, n_heads=65536, q_stride=1 << 22, q_out_stride=1 << 22) == B.WISV_EUNSUPPORTED
+        assert append(n_tokens=0, slots=None, q=None) == 0       # nothing to do
+        assert lib.wisv_paged_append(h, None) == B.WISV_EINVAL and lib.wisv_paged_append(None, None) == B.WISV_EINVAL
+        assert log() == []
+        assert append(n_heads=0, q=None, q_out=None, cos=None, sin=None, positions=None) == 0 and len(log()) == 1
+        assert append(q_out=P) == 0 and append(dtype=0, q_stride=260, k_stride=132) == 0
+    ''')
+
+
+def test_attention_refuses_bad_arguments(stub):
+    run(stub, '''
+        assert need() == 0 and attn() == 0 and log(), text()
+        stub.stub_log_clear()
+        for kw, what in ((dict(batch=-1), "batch"), (dict(n_tokens=-1), "n_tokens"), (dict(n_heads=3), "n_heads"), (dict(n_heads=0), "n_heads"),
+                         (dict(n_kv_heads=0), "n_kv_heads"), (dict(head_dim=80), "head_dim"), (dict(dtype=-1), "dtype"), (dict(page_size=100), "page_size"),
+                         (dict(max_pages=0), "max_pages"), (dict(max_pages=2**31 - 1), "max_pages"), (dict(max_new=-1), "max_new"), (dict(max_len=-1), "max_len"),
+                         (dict(window=-1), "window"), (dict(softcap=-1.0), "softcap"), (dict(softcap=float("nan")), "softcap"),
+                         (dict(softcap=float("inf")), "softcap"), (dict(scale=float("inf")), "scale"), (dict(q=None), "q and out"), (dict(out=P + 4), "q and out"),
+                         (dict(q_stride=128), "q and out"), (dict(out_stride=257), "q and out"), (dict(block_table=None), "NULL"), (dict(q_start=None), "NULL"),
+                         (dict(kv_len=None), "NULL"), (dict(page_stride=8), "page_stride")):
+            assert attn(**kw) == B.WISV_EINVAL and what in text(), (kw, text())
+            n = C.c_size_t()
+            assert lib.wisv_paged_attention_workspace(h, C.byref(attn_args(**kw)), C.byref(n)) == B.WISV_EINVAL
+        big = 2**31 - 1
+        assert attn(n_tokens=big) == B.WISV_EUNSUPPORTED
+        assert lib.wisv_paged_attention(h, None) == B.WISV_EINVAL and lib.wisv_paged_attention(None, None) == B.WISV_EINVAL
+        assert lib.wisv_paged_attention_workspace(h, C.byref(attn_args()), None) == B.WISV_EINVAL
+        assert attn(batch=0, q=None) == 0 and attn(n_tokens=0, block_table=None) == 0     # nothing to do
+        # a cache that is worth cutting needs room for its parts
+        long = dict(batch=1, n_tokens=1, max_pages=4096, max_len=65536, max_new=1)
+        n = need(**long)
+        assert n > 0
+        for kw in (dict(), dict(workspace=P, workspace_bytes=n - 1), dict(workspace=P + 4, workspace_bytes=n), dict(workspace_bytes=n)):
+            assert attn(**long, **kw) == B.WISV_EINVAL and "workspace" in text(), kw
+        assert log() == []
+        assert attn(**long, workspace=P, workspace_bytes=n) == 0 and any("join" in l for l in log())
+    ''')
+
+
+def test_struct_sizes_match_the_header_layout():
+    import ctypes as C
+    assert C.sizeof(binding.wisv_paged_plan_args) == 5 * 4 + 4 + 11 * 8
+    assert C.sizeof(binding.wisv_paged_append_args) == 8 * 4 + 4 * 8 + 4 * 8 + 6 * 8 + 2 * 8
+    assert C.sizeof(binding.wisv_paged_attention_args) == 14 * 4 + 4 * 8 + 3 * 8 + 6 * 8 + 2 * 8
+
+
+def test_paged_fill_follows_the_documented_layout():
+    kp, vp = binding.new_paged_cache(5, 2, 16, 32, torch.float32, "cpu")
+    k, v = torch.randn(2, 37, 32), torch.randn(2, 37, 32)
+    binding.paged_fill(kp, vp, [4, 0, 2], k, v)
+    for pos in (0, 7, 8, 15, 16, 31, 36):
+        page = [4, 0, 2][pos // 16]
+        for d in (0, 5, 31):
+            flat = vp[page, 1].reshape(-1)
+            assert kp[page, 1, pos % 16, d] == k[1, pos, d] and flat[((pos % 16) // 8 * 32 + d) * 8 + pos % 8] == v[1, pos, d]
+    assert float(kp[1].abs().sum() + kp[3].abs().sum() + kp[2, :, 5:].abs().sum()) == 0.0
+    gk, gv, there = ref.gather(kp.double().numpy(), vp.double().numpy(), [4, 0, 2], 37)
+    assert there.all() and np.array_equal(gk, k.double().numpy()) and np.array_equal(gv, v.double().numpy())
+
+
+def test_oracle_plan_by_hand():
+    # 3 of a page's 4 positions held, 2 more: one new page; idle; 8 held in a full table row: refused; 5 new: two pages
+    got = ref.plan([3, 0, 8, 0], [2, 0, 1, 5], [9, 8, 7], [[5, -1], [-1, -1], [1, 2], [-1, -1]], 4, 9)
+    q_start, kv_len, positions, slots, used, status, table = got
+    assert q_start.tolist() == [0, 2, 2, 3, 8] and kv_len.tolist() == [5, 0, 8, 5]
+    assert positions.tolist() == [3, 4, 8, 0, 1, 2, 3, 4, 0]
+    assert slots[:2].tolist() == [5 * 4 + 3, 9 * 4] and slots[2] == -1            # the third request's row is full
+    assert status.tolist() == [0, 0, 2, 0] and table[3].tolist() == [8, 7] and used.tolist() == [3]
+    assert slots[3:8].tolist() == [32, 33, 34, 35, 28] and slots[8] == -1
+
+
+def test_oracle_attention_by_hand():
+    """Two keys with scores 0 and ln 3: weights 1/4 and 3/4; a window of one, a cap, a bias and a prefix change them as written."""
+    kp, vp = np.zeros((1, 1, 16, 2)), np.zeros((1, 1, 2, 2, 8))
+    kp[0, 0, 1] = [np.log(3.0), 0.0]
+    vp[0, 0, 0, :, 0], vp[0, 0, 0, :, 1] = [4.0, 0.0], [0.0, 4.0]
+    q = np.array([[[1.0, 0.0]]])
+    call = lambda **kw: ref.attention(q, kp, vp, [[0]], [0, 1], [2], scale=1.0, **kw)[0][0, 0].tolist()  # noqa: E731
+    assert np.allclose(call(), [1.0, 3.0])
+    assert np.allclose(call(window=1), [0.0, 4.0])
+    assert np.allclose(call(window=1, prefix=[1]), [1.0, 3.0])
+    cap = 2 * np.tanh(np.log(3.0) / 2)                                            # = 1
+    assert np.allclose(cap, 1.0) and np.allclose(call(softcap=2.0), [4 / (1 + np.e), 4 * np.e / (1 + np.e)])
+    assert np.allclose(call(slopes=[np.log(3.0)]), [0.4, 3.6])                    # the nearer key gains another factor of 3
+    out = ref.attention(np.ones((3, 1, 2)), kp, vp, [[0]], [0, 3], [2], scale=1.0)[0]
+    assert (out[0] == 0).all() and np.allclose(out[1, 0], [4.0, 0.0])             # the first row lies before the cache
