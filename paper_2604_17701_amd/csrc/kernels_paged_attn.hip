@@ -51,11 +51,7 @@ __device__ __forceinline__ StepPages step_pages(const PagedAttn &a, const int32_
     return s;
 }
 
-// A float that is no number or infinite has all exponent bits set
-template <typename T> __device__ __forceinline__ bool any_not_finite(uint32_t w) {
-    if (sizeof(T) == 2) return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-    return (w & 0x7f800000u) == 0x7f800000u;
-}
+constexpr int NW = 4;   // waves of a workgroup of k_paged_rows
 
 constexpr int merge_tiles(int nw, int nq, int dt) {   // feature tiles of 16 joined at a time: at most 32 KB of LDS
     int d = dt;
@@ -63,7 +59,7 @@ constexpr int merge_tiles(int nw, int nq, int dt) {   // feature tiles of 16 joi
     return d;
 }
 
-template <typename T, int HD, int NQ, int NW, bool MODS>
+template <typename T, int HD, int NQ, bool MODS>
 __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
     constexpr int KEYS = Step<T>::KEYS, E = Step<T>::E, KL = HD / 16, QL = HD * (int)sizeof(T) / 64, DT = HD / 16;
     constexpr int DP = merge_tiles(NW, NQ, DT);
@@ -88,9 +84,8 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
         const int rho_end = min(rho0 + 16 * NQ, R);
         const int pos_min = rq.pos0 + rho0 / a.rep, pos_max = rq.pos0 + (rho_end - 1) / a.rep;
         const PagedSteps st = paged_steps(rq, pos_min, pos_max, a.window, KEYS);
-        int s = split * a.split_steps;
-        const int s_end = split == a.n_splits - 1 ? st.total : min(st.total, s + a.split_steps);
-        s += wave;
+        const int s_begin = split * a.split_steps, s_end = split == a.n_splits - 1 ? st.total : min(st.total, s_begin + a.split_steps);
+        int s = s_begin + wave;
 
         // queries: operand (nq, t) of lane (bj, bg) holds 16 bytes of row rho0 + 16 nq + bj
         paged_u4 q[NQ][QL];
@@ -136,6 +131,12 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                 for (int dt = 0; dt < DT; ++dt) va[dt] = *reinterpret_cast<const paged_u4 *>(src + dt * 128);
             };
             auto real = [&](int v) { return v < st.n_pre ? v : v + st.skip; };
+            // whether every row sees every key of the step (the same for the whole wave)
+            auto see_all = [&](int key0, const StepPages &p) {
+                return p.has[0] && p.has[1] && key0 + KEYS <= rq.n_keys &&
+                       (key0 + KEYS <= rq.prefix || (key0 + KEYS - 1 <= pos_min && (!a.window || key0 > pos_max - a.window)));
+            };
+            uint32_t odd = 0;   // bits of values that are not finite, of steps that not every row sees
             StepPages cur = step_pages<T, HD>(a, table, g, real(s));
             load_k(cur);
             load_v(cur);
@@ -143,9 +144,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
             for (; s < s_end; s += NW) {
                 const int step = real(s), key0 = step * KEYS, kbase = key0 + E * bg;   // this lane's keys: kbase .. kbase + E - 1
                 const int n_mine = (vrun ? cur.has[1] : cur.has[0]) ? rq.n_keys : 0;   // keys in a hole of the table are not there
-                // whether every row sees every key of the step (the same for the whole wave)
-                const bool whole = cur.has[0] && cur.has[1] && key0 + KEYS <= rq.n_keys &&
-                                   (key0 + KEYS <= rq.prefix || (key0 + KEYS - 1 <= pos_min && (!a.window || key0 > pos_max - a.window)));
+                const bool whole = see_all(key0, cur);
                 paged_u4 phi[NQ], plo[NQ];   // float: phi holds the four probabilities themselves
 #pragma unroll
                 for (int nq = 0; nq < NQ; ++nq) {
@@ -177,12 +176,11 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                         x[e] = v * 1.4426950408889634f;   // in units of ln 2: every exponential is one instruction
                     }
                     if (!whole) {
-                        const int lo = a.window ? pos[nq] - a.window : -1;   // (no window: below every key)
+                        const int lo = a.window ? pos[nq] - a.window : -1;
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
                             const int j = kbase + e;
-                            const bool sees = j < n_mine && (j < rq.prefix || (j <= pos[nq] && j > lo));
-                            x[e] = sees ? x[e] : -INFINITY;
+                            x[e] = paged_sees(j, n_mine, rq.prefix, pos[nq], lo) ? x[e] : -INFINITY;
                         }
                     }
                     float mx = x[0];
@@ -219,19 +217,10 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                     }
                 }
                 load_k(nxt);
-                auto add_v = [&](const paged_u4 &v, int nq, paged_f4 o) {
-                    if (BF) {
-                        o = mfma_bf16(v, phi[nq], o);
-                        return mfma_bf16(v, plo[nq], o);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o = mfma_f32(v[j], phi[nq][j], o);
-                    return o;
-                };
-                bool odd = false;
                 if (!whole) {
-                    // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN
-                    // would reach every row.  The same holds for values that only some rows see.
+                    // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN would
+                    // reach every row.  The same holds for values that only some rows see: those that are not finite are
+                    // taken out here and added below.
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -239,44 +228,50 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                             uint32_t keep;
                             if (BF) keep = (kbase + 2 * e < n_mine ? 0xffffu : 0u) | (kbase + 2 * e + 1 < n_mine ? 0xffff0000u : 0u);
                             else keep = kbase + e < n_mine ? 0xffffffffu : 0u;
-                            va[dt][e] &= keep;
-                            odd |= any_not_finite<T>(va[dt][e]);
+                            const uint32_t w = va[dt][e] & keep;
+                            const uint32_t fine = BF ? finite_halves(w) : (w & 0x7f800000u) != 0x7f800000u ? 0xffffffffu : 0u;
+                            odd |= w & ~fine;
+                            va[dt][e] = w & fine;
                         }
-                    odd = __any(odd);
                 }
-                if (!odd) {
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int nq = 0; nq < NQ; ++nq) oacc[nq][dt] = add_v(va[dt], nq, oacc[nq][dt]);
-                } else {
-                    // a value that is not finite among keys that some row does not see: one key at a time, added only
-                    // to the rows that see it
-                    for (int k = 0; k < KEYS; ++k) {
-                        const int e = k % E, j = key0 + k;
-                        const bool mine = bg == k / E;
-                        const bool there = (k < HALF ? cur.has[0] : cur.has[1]) && j < rq.n_keys;
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        if (BF) {
+                            oacc[nq][dt] = mfma_bf16(va[dt], phi[nq], oacc[nq][dt]);
+                            oacc[nq][dt] = mfma_bf16(va[dt], plo[nq], oacc[nq][dt]);
+                        } else {
 #pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            paged_u4 one;
-#pragma unroll
-                            for (int w = 0; w < 4; ++w) {
-                                if (BF) one[w] = mine && w == e / 2 ? va[dt][w] & (e & 1 ? 0xffff0000u : 0xffffu) : 0u;
-                                else one[w] = mine && w == e ? va[dt][w] : 0u;
-                            }
-#pragma unroll
-                            for (int nq = 0; nq < NQ; ++nq) {
-                                const bool sees = there && (j < rq.prefix || (j <= pos[nq] && (!a.window || j > pos[nq] - a.window)));
-                                const paged_f4 o = add_v(one, nq, oacc[nq][dt]);
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) oacc[nq][dt][r] = sees ? o[r] : oacc[nq][dt][r];
-                            }
+                            for (int j = 0; j < 4; ++j) oacc[nq][dt] = mfma_f32(va[dt][j], phi[nq][j], oacc[nq][dt]);
                         }
                     }
-                }
                 load_v(nxt);
                 cur = nxt;
                 nxt = step_pages<T, HD>(a, table, g, real(min(s + 2 * NW, s_end - 1)));
+            }
+            if (__any(odd != 0)) {
+                // rare: some value of a step that not every row sees is not finite.  Each row takes those that it sees
+#pragma unroll 1
+                for (s = s_begin + wave; s < s_end; s += NW) {
+                    const int key0 = real(s) * KEYS;
+                    const StepPages sp = step_pages<T, HD>(a, table, g, real(s));
+                    if (see_all(key0, sp)) continue;
+#pragma unroll 1
+                    for (int j = key0; j < min(key0 + KEYS, rq.n_keys); ++j) {
+                        const int run = j - key0 >= HALF, in = j - key0 - run * HALF;   // (a run of keys begins a group of eight)
+                        if (!sp.has[run]) continue;
+                        const T *v = vpool + sp.at[run] + (in & ~7) * HD + (in & 7) + 32 * bg;
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) {
+                            if (!paged_sees(j, rq.n_keys, rq.prefix, pos[nq], a.window ? pos[nq] - a.window : -1)) continue;
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) oacc[nq][dt][r] += only_not_finite(v[(16 * dt + r) * 8]);
+                        }
+                    }
+                }
             }
         }
 
@@ -385,44 +380,73 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
 
 // ------------------------------------------------------------------------------------------ launch
 
-constexpr int NW = 4;
+// rows of a request that k_paged_rows reads the keys once for
+constexpr int ROW_LIMIT = 32;
 
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len) {
-    const int keys = bf16 ? 32 : 16, steps = (max_len + keys - 1) / keys, wgs = std::max(1, a.batch * a.G);
     PagedCut c;
-    c.n_splits = std::max(1, std::min(std::min(512 / wgs, (steps + NW - 1) / NW), PAGED_MAX_SPLITS));
+    c.prompt = bf16 && (int64_t)a.rep * max_new > ROW_LIMIT;
+    c.rows = !c.prompt || a.batch > 1;
+    const int steps = (max_len + 63) / 64;
+    int64_t wgs;
+    if (c.prompt) {
+        // a prompt's workgroups are as many as its tiles, one to a CU; splits only where most CUs would have none
+        wgs = (int64_t)paged_prompt_tiles(a, head_dim) * a.G;
+        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 / std::max<int64_t>(wgs, 1), (steps + 3) / 4), PAGED_MAX_SPLITS));
+    } else {
+        wgs = (int64_t)a.batch * a.G;
+        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(wgs, 1), (steps * 2 + NW - 1) / NW), PAGED_MAX_SPLITS));
+    }
     c.workspace = c.n_splits == 1 ? 0 : (size_t)c.n_splits * a.n_tokens * a.H * (head_dim + 2) * 4;
     return c;
 }
 
 template <typename T, int HD, int NQ> static void launch_rows(const PagedAttn &a, hipStream_t stream) {
     const dim3 grid(a.batch * a.G, a.n_splits);
-    if (a.softcap > 0.f || a.slopes) hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, NW, true>), grid, dim3(64 * NW), 0, stream, a);
-    else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, NW, false>), grid, dim3(64 * NW), 0, stream, a);
+    if (a.softcap > 0.f || a.slopes) hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, true>), grid, dim3(64 * NW), 0, stream, a);
+    else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, false>), grid, dim3(64 * NW), 0, stream, a);
 }
-template <typename T, int HD> static void launch_attn_t(const PagedAttn &a, int max_new, hipStream_t stream) {
-    if ((int64_t)a.rep * max_new <= 16) launch_rows<T, HD, 1>(a, stream);
+template <typename T, int HD> static void launch_rows_t(const PagedAttn &a, int rows, hipStream_t stream) {
+    if (rows <= 16) launch_rows<T, HD, 1>(a, stream);
     else launch_rows<T, HD, 2>(a, stream);
-    if (a.n_splits > 1)
-        hipLaunchKernelGGL((k_paged_join<T, HD>), dim3((unsigned)(((int64_t)a.n_tokens * a.H + 3) / 4)), dim3(256), 0, stream, a);
 }
-template <typename T> static void launch_attn_d(const PagedAttn &a, int head_dim, int max_new, hipStream_t stream) {
+template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim, int rows, hipStream_t stream) {
     switch (head_dim) {
-        case 32: return launch_attn_t<T, 32>(a, max_new, stream);
-        case 64: return launch_attn_t<T, 64>(a, max_new, stream);
-        case 128: return launch_attn_t<T, 128>(a, max_new, stream);
-        default: return launch_attn_t<T, 256>(a, max_new, stream);
+        case 32: return launch_rows_t<T, 32>(a, rows, stream);
+        case 64: return launch_rows_t<T, 64>(a, rows, stream);
+        case 128: return launch_rows_t<T, 128>(a, rows, stream);
+        default: return launch_rows_t<T, 256>(a, rows, stream);
+    }
+}
+template <typename T> static void launch_join(const PagedAttn &a, int head_dim, hipStream_t stream) {
+    const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.H + 3) / 4));
+    switch (head_dim) {
+        case 32: hipLaunchKernelGGL((k_paged_join<T, 32>), grid, dim3(256), 0, stream, a); break;
+        case 64: hipLaunchKernelGGL((k_paged_join<T, 64>), grid, dim3(256), 0, stream, a); break;
+        case 128: hipLaunchKernelGGL((k_paged_join<T, 128>), grid, dim3(256), 0, stream, a); break;
+        default: hipLaunchKernelGGL((k_paged_join<T, 256>), grid, dim3(256), 0, stream, a); break;
     }
 }
 
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream) {
-    (void)device;
-    a.n_splits = paged_cut(a, bf16, head_dim, max_new, max_len).n_splits;
-    const int keys = bf16 ? 32 : 16, steps = (max_len + keys - 1) / keys;
-    a.split_steps = std::max(1, (steps + a.n_splits - 1) / a.n_splits);
-    a.row_limit = 0;
-    if (bf16) launch_attn_d<bf16_t>(a, head_dim, max_new, stream);
-    else launch_attn_d<float>(a, head_dim, max_new, stream);
+    const PagedCut cut = paged_cut(a, bf16, head_dim, max_new, max_len);
+    a.n_splits = cut.n_splits;
+    a.row_limit = cut.rows && cut.prompt ? ROW_LIMIT : 0;
+    const auto per_split = [&](int step) { return std::max(1, ((max_len + step - 1) / step + a.n_splits - 1) / a.n_splits); };
+    if (cut.prompt) {
+        a.split_steps = per_split(64);
+        if (const char *why = launch_paged_prompt(a, head_dim, device, stream)) return why;
+    }
+    if (cut.rows) {
+        a.split_steps = per_split(bf16 ? 32 : 16);
+        const int rows = (int)std::min<int64_t>((int64_t)a.rep * max_new, ROW_LIMIT);
+        if (bf16) launch_rows_d<bf16_t>(a, head_dim, rows, stream);
+        else launch_rows_d<float>(a, head_dim, rows, stream);
+    }
+    if (a.n_splits > 1) {
+        if (bf16) launch_join<bf16_t>(a, head_dim, stream);
+        else launch_join<float>(a, head_dim, stream);
+    }
     return nullptr;
 }
 

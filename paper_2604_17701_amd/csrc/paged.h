@@ -38,10 +38,15 @@ struct PagedAttn {
 constexpr int PAGED_MAX_SPLITS = 64;   // the kernel that joins them gives each a lane
 // What a call will launch, from the sizes and the hints alone
 struct PagedCut {
+    bool rows, prompt;             // k_paged_rows, k_paged_prompt (both: requests go by row_limit)
     int n_splits;
     size_t workspace;              // bytes
 };
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len);
+// The kernel of many rows (bf16): its rows per tile and how many tiles a call has at most
+int paged_prompt_rows(int head_dim);
+int paged_prompt_tiles(const PagedAttn &a, int head_dim);
+const char *launch_paged_prompt(const PagedAttn &a, int head_dim, int device, hipStream_t stream);
 // null, or why the launch failed
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream);
 
@@ -85,6 +90,22 @@ __device__ __forceinline__ PagedSteps paged_steps(const PagedRequest &r, int pos
     t.skip = first - t.n_pre;
     t.total = t.n_pre + max(last - first, 0);
     return t;
+}
+
+// Whether a row at position pos sees key j of n keys; lo: the position before its window, -1 without one.  (No && or ||: a
+// branch per score costs more than the comparisons.)
+__device__ __forceinline__ bool paged_sees(int j, int n, int prefix, int pos, int lo) {
+    return bool((int)(j < n) & ((int)(j < prefix) | ((int)(j <= pos) & (int)(j > lo))));
+}
+
+// Two bf16 values: the halves that are finite, all bits of each
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    return ((w & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u);
+}
+// the value if it is infinite or no number, else 0
+template <typename T> __device__ __forceinline__ float only_not_finite(T bits) {
+    const float v = Elem<T>::load(&bits);
+    return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? v : 0.f;
 }
 
 // tanh for scores that end in bf16: an absolute error of about 2^-23
