@@ -340,42 +340,69 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
     }
 }
 
-// out = sum_s 2^(m_s - m*) o_s / sum_s 2^(m_s - m*) l_s over the splits that saw a key, in split order.  One wave per
-// (row, head): lane s holds the weight of split s, then every lane adds up its features.
-template <typename T, int HD>
+// out = sum_s 2^(m_s - m*) o_s / sum_s 2^(m_s - m*) l_s over the splits that saw a key.  A thread owns four features of a (row,
+// head) and every GROUPS-th split, four of which are on their way at a time; the groups' sums are added in order.  GROUPS 1 fills
+// the chip when there are many rows, the whole workgroup on one (row, head) is for few rows of many splits.
+template <typename T, int HD, int GROUPS>
 __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
-    constexpr int N = HD >= 128 ? HD / 64 : 1;   // features per lane (HD 32: half of the lanes have none)
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = item / a.H;
+    constexpr int TPI = HD / 4, ITEMS = 256 / (TPI * GROUPS), AHEAD = 4;
+    __shared__ float sm[GROUPS][TPI * ITEMS], sd[GROUPS][TPI * ITEMS];
+    __shared__ paged_f4 sa[GROUPS][TPI * ITEMS];
+    const int tid = threadIdx.x, group = tid / (TPI * ITEMS), in = tid % (TPI * ITEMS), d = in % TPI * 4;
+    const int64_t item = (int64_t)blockIdx.x * ITEMS + in / TPI, row = item / a.H;
     const int h = item % a.H;
-    if (row >= min(a.q_start[a.batch], a.n_tokens)) return;   // rows behind the last request stay as they are
-    const int64_t at = row * a.H + h, step = (int64_t)a.n_tokens * a.H;
-    const bool mine = lane < a.n_splits;
-    const float m = mine ? a.pm[at + lane * step] : -INFINITY, l = mine ? a.pl[at + lane * step] : 0.f;
-    const float top = wave_max(l != 0.f ? m : -INFINITY);
-    const float w = l != 0.f ? __builtin_amdgcn_exp2f(m - top) : 0.f;
-    const float den = wave_sum(w * l);
-    float acc[N];
+    const bool live = row < min(a.q_start[a.batch], a.n_tokens);   // rows behind the last request stay as they are
+    if (GROUPS == 1 && !live) return;
+    const int64_t at = (live ? row : 0) * a.H + h, step = (int64_t)a.n_tokens * a.H;
+    float mx = -INFINITY, den = 0.f;
+    paged_f4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = group; s0 < a.n_splits; s0 += GROUPS * AHEAD) {
+        float m[AHEAD], l[AHEAD];
+        paged_f4 o[AHEAD];
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    const int d = lane * N;
-    unsigned long long seen = __ballot(l != 0.f);
-    while (seen) {
-        const int s = __ffsll(seen) - 1;
-        seen &= seen - 1;
-        const float ws = __shfl(w, s, 64);
-        if (d < HD) {
-            const float *src = a.po + (at + s * step) * HD + d;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t from = at + min(s0 + i * GROUPS, a.n_splits - 1) * step;   // (splits past the last re-read it and count as none)
+            m[i] = a.pm[from];
+            l[i] = s0 + i * GROUPS < a.n_splits ? a.pl[from] : 0.f;
+            o[i] = *reinterpret_cast<const paged_f4 *>(a.po + from * HD + d);
+        }
+        float top = mx;
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] = fmaf(ws, src[i], acc[i]);
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, l[i] != 0.f ? m[i] : -INFINITY);
+        if (top == -INFINITY) continue;
+        const float keep = __builtin_amdgcn_exp2f(mx - top);
+        den *= keep;
+        acc *= keep;
+        mx = top;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (l[i] == 0.f) continue;   // (a split without keys has written no output)
+            const float w = __builtin_amdgcn_exp2f(m[i] - top);
+            den = fmaf(w, l[i], den);
+            acc += o[i] * w;
         }
     }
-    if (d >= HD) return;
-    const float inv = den == 0.f ? 0.f : 1.f / den;
+    if (GROUPS > 1) {
+        sm[group][in] = mx;
+        sd[group][in] = den;
+        sa[group][in] = acc;
+        __syncthreads();
+        if (group || !live) return;
+        float top = -INFINITY;
+        for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, sm[i][in]);
+        const float sub = top == -INFINITY ? 0.f : top;
+        den = 0.f;
+        acc = paged_f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < GROUPS; ++i) {
+            const float w = __builtin_amdgcn_exp2f(sm[i][in] - sub);
+            den = fmaf(w, sd[i][in], den);
+            acc += sa[i][in] * w;
+        }
+    }
+    acc *= den == 0.f ? 0.f : 1.f / den;
     T *dst = (T *)a.out + row * a.out_stride + (int64_t)h * HD + d;
-#pragma unroll
-    for (int i = 0; i < N; ++i) Elem<T>::store(dst + i, acc[i] * inv);
+    if (sizeof(T) == 2) *reinterpret_cast<uint2 *>(dst) = make_uint2(f32x2_to_bf16x2(acc[0], acc[1]), f32x2_to_bf16x2(acc[2], acc[3]));
+    else *reinterpret_cast<paged_f4 *>(dst) = acc;
 }
 
 // ------------------------------------------------------------------------------------------ launch
@@ -387,16 +414,26 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     PagedCut c;
     c.prompt = bf16 && (int64_t)a.rep * max_new > ROW_LIMIT;
     c.rows = !c.prompt || a.batch > 1;
-    const int steps = (max_len + 63) / 64;
-    int64_t wgs;
+    // positions that a tile's rows see at most: a window's are those of its first row and what its rows span
+    const int reach = a.window ? (int)std::min<int64_t>(max_len, (int64_t)a.window + 64 + (c.prompt ? 128 / a.rep : max_new)) : max_len;
+    const int64_t steps = (reach + 63) / 64;
     if (c.prompt) {
-        // a prompt's workgroups are as many as its tiles, one to a CU; splits only where most CUs would have none
-        wgs = (int64_t)paged_prompt_tiles(a, head_dim) * a.G;
-        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 / std::max<int64_t>(wgs, 1), (steps + 3) / 4), PAGED_MAX_SPLITS));
+        // Workgroups run two to a CU (head_dim 256: one).  Splitting the keys fills a chip, or the last of its rounds, that is not
+        // full.  In steps of 64 keys, about 2 us each: a split costs six (its start, its way to the join), the join three and
+        // the parts' way through memory
+        const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = head_dim == 256 ? 256 : 512;
+        const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;
+        double best = 0;
+        c.n_splits = 1;
+        for (int s = 1; s <= 16 && (s == 1 || steps / s >= 4); ++s) {
+            const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + 0.25) * ((double)steps / s + 6) + (s > 1 ? 3 + s * part : 0);
+            if (s == 1 || cost < best) best = cost, c.n_splits = s;
+        }
     } else {
-        wgs = (int64_t)a.batch * a.G;
-        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(wgs, 1), (steps * 2 + NW - 1) / NW), PAGED_MAX_SPLITS));
+        const int64_t wgs = std::max<int64_t>(1, (int64_t)a.batch * a.G);
+        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / wgs, (steps * 2 + NW - 1) / NW), PAGED_MAX_SPLITS));
     }
+    c.split_steps = (int)((steps + c.n_splits - 1) / c.n_splits);
     c.workspace = c.n_splits == 1 ? 0 : (size_t)c.n_splits * a.n_tokens * a.H * (head_dim + 2) * 4;
     return c;
 }
@@ -418,13 +455,18 @@ template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim
         default: return launch_rows_t<T, 256>(a, rows, stream);
     }
 }
+template <typename T, int HD> static void launch_join_t(const PagedAttn &a, hipStream_t stream) {
+    constexpr int ALL = 1024 / HD;   // groups that a workgroup has for one (row, head)
+    const int64_t items = (int64_t)a.n_tokens * a.H;
+    if (a.n_splits > 8) hipLaunchKernelGGL((k_paged_join<T, HD, ALL>), dim3((unsigned)items), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((k_paged_join<T, HD, 1>), dim3((unsigned)((items + ALL - 1) / ALL)), dim3(256), 0, stream, a);
+}
 template <typename T> static void launch_join(const PagedAttn &a, int head_dim, hipStream_t stream) {
-    const dim3 grid((unsigned)(((int64_t)a.n_tokens * a.H + 3) / 4));
     switch (head_dim) {
-        case 32: hipLaunchKernelGGL((k_paged_join<T, 32>), grid, dim3(256), 0, stream, a); break;
-        case 64: hipLaunchKernelGGL((k_paged_join<T, 64>), grid, dim3(256), 0, stream, a); break;
-        case 128: hipLaunchKernelGGL((k_paged_join<T, 128>), grid, dim3(256), 0, stream, a); break;
-        default: hipLaunchKernelGGL((k_paged_join<T, 256>), grid, dim3(256), 0, stream, a); break;
+        case 32: return launch_join_t<T, 32>(a, stream);
+        case 64: return launch_join_t<T, 64>(a, stream);
+        case 128: return launch_join_t<T, 128>(a, stream);
+        default: return launch_join_t<T, 256>(a, stream);
     }
 }
 
@@ -432,13 +474,12 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
     const PagedCut cut = paged_cut(a, bf16, head_dim, max_new, max_len);
     a.n_splits = cut.n_splits;
     a.row_limit = cut.rows && cut.prompt ? ROW_LIMIT : 0;
-    const auto per_split = [&](int step) { return std::max(1, ((max_len + step - 1) / step + a.n_splits - 1) / a.n_splits); };
     if (cut.prompt) {
-        a.split_steps = per_split(64);
+        a.split_steps = cut.split_steps;
         if (const char *why = launch_paged_prompt(a, head_dim, device, stream)) return why;
     }
     if (cut.rows) {
-        a.split_steps = per_split(bf16 ? 32 : 16);
+        a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
         const int rows = (int)std::min<int64_t>((int64_t)a.rep * max_new, ROW_LIMIT);
         if (bf16) launch_rows_d<bf16_t>(a, head_dim, rows, stream);
         else launch_rows_d<float>(a, head_dim, rows, stream);

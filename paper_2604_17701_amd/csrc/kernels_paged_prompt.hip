@@ -29,32 +29,25 @@ __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, co
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
 }
 
-// waves of a workgroup, and what they leave of a SIMD's registers: two waves per SIMD overlap one's softmax with the other's
-// products; head_dim 256 needs the registers of one
-constexpr int prompt_waves(int hd) { return hd == 256 ? 4 : 8; }
-constexpr size_t prompt_lds(int hd) { return (size_t)2 * 2 * BLOCK * hd * 2; }
+constexpr int PROMPT_WAVES = 4;
+// Blocks in LDS, 64 KB or (head_dim 256, whose registers allow one workgroup per CU) 128
+constexpr int prompt_stages(int hd) { return hd == 256 ? 2 : 256 / hd; }
+constexpr size_t prompt_lds(int hd) { return (size_t)prompt_stages(hd) * 2 * BLOCK * hd * 2; }
+enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 
-template <int HD, bool MODS>
-__global__ __launch_bounds__(64 * prompt_waves(HD), HD == 256 ? 1 : 2) void k_paged_prompt(PagedAttn a) {
-    extern __shared__ __align__(16) unsigned char lds[];   // [2 buffers][K, V][BLOCK * HD]
-    constexpr int NWV = prompt_waves(HD), ROWS = 32 * NWV, CPR = HD / 8, QT = HD / 16, OT = HD / 32;
-    constexpr int HALF = BLOCK * HD * 2, BUF = 2 * HALF;                               // bytes
-    constexpr int KW = BLOCK / NWV > 512 / HD ? BLOCK / NWV : 512 / HD;                // positions a wave fetches
-    constexpr int PIECES = KW * HD * 2 / 1024;
+template <int HD, int MODS>
+__global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_prompt(PagedAttn a) {
+    extern __shared__ __align__(16) unsigned char lds[];   // [STAGES][K, V][BLOCK * HD]
+    constexpr int NWV = PROMPT_WAVES, ROWS = 32 * NWV, CPR = HD / 8, QT = HD / 16, OT = HD / 32, STAGES = prompt_stages(HD);
+    constexpr float LOG2E = 1.4426950408889634f;
+    constexpr int HALF = BLOCK * HD * 2, BUF = 2 * HALF;               // bytes
+    constexpr int LOADS = HD / 32, WAITS = 2 * LOADS;                  // loads of 1 KB that sixteen positions take of either pool, and of both
+    static_assert(STAGES >= 2 && (STAGES - 2) * WAITS <= 63, "vmcnt holds six bits");
     const int tid = threadIdx.x, lane = tid & 63, h2 = lane >> 5, qi = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = blockIdx.x % a.G, split = blockIdx.y;
     const int tile = gridDim.x / a.G - 1 - blockIdx.x / a.G;   // later rows see more keys: they start first
-
-    // ---- whose tile this is: request b owns the tiles from floor(q_start[b] rep / ROWS) + b on
-    int b = 0;
-    for (int n = a.batch; n > 1;) {
-        const int stride = (n + 63) / 64, at = lane * stride;
-        const bool before = at < n && (int64_t)min(max(a.q_start[b + min(at, n - 1)], 0), a.n_tokens) * a.rep / ROWS + b + at <= tile;
-        const int k = max(__popcll(__ballot(before)) - 1, 0);
-        b = __builtin_amdgcn_readfirstlane(b + k * stride);
-        n = __builtin_amdgcn_readfirstlane(min(stride, n - k * stride));
-    }
+    const int b = paged_find(a, tile, ROWS, lane);
     const PagedRequest rq = paged_request(a, b);
     const int R = rq.n_new * a.rep;
     const int64_t first = (int64_t)rq.row0 * a.rep / ROWS + b;
@@ -62,15 +55,20 @@ __global__ __launch_bounds__(64 * prompt_waves(HD), HD == 256 ? 1 : 2) void k_pa
     const int rho0 = (int)(tile - first) * ROWS;
     const PagedSteps st = paged_steps(rq, rq.pos0 + rho0 / a.rep, rq.pos0 + (min(rho0 + ROWS, R) - 1) / a.rep, a.window, BLOCK);
     const int s_begin = split * a.split_steps, s_end = split == a.n_splits - 1 ? st.total : min(st.total, s_begin + a.split_steps);
-    const int32_t *table = a.block_table + (int64_t)b * a.max_pages;
+    // (the table is read through the scalar cache: a vector load's wait would be one for the loads on their way to LDS)
+    typedef const int32_t __attribute__((address_space(4))) *const_ints;
+    const const_ints table = (const_ints)(uintptr_t)(a.block_table + (int64_t)b * a.max_pages);
+    const auto real = [&](int v) { return v < st.n_pre ? v : v + st.skip; };
+
+    const int tile_min = rq.pos0 + rho0 / a.rep, tile_max = rq.pos0 + (min(rho0 + ROWS, R) - 1) / a.rep;
 
     // ---- this wave's rows
     const int wrow = rho0 + 32 * wave;
     const bool busy = wrow < R;
-    const int rho = min(wrow + qi, R - 1), tok = rho / a.rep, head = g * a.rep + rho % a.rep;
-    const int pos = rq.pos0 + tok, pos_min = rq.pos0 + min(wrow, R - 1) / a.rep, pos_max = rq.pos0 + min(wrow + 31, R - 1) / a.rep;
-    const int lo = a.window ? pos - a.window : -1;   // keys at or below it lie outside the window
-    const float slope = MODS && a.slopes ? a.slopes[head] : 0.f;
+    const int pos_min = rq.pos0 + min(wrow, R - 1) / a.rep, pos_max = rq.pos0 + min(wrow + 31, R - 1) / a.rep;
+    const int rho = min(wrow + qi, R - 1), tok = rho / a.rep, head = g * a.rep + rho % a.rep, pos = rq.pos0 + tok;
+    const int lo = a.window ? pos - a.window : -1;   // the position before the window
+    const float slope = (MODS & BIAS) && a.slopes ? a.slopes[head] * LOG2E : 0.f;
     paged_u4 q[QT];   // lane: features 16 t + 8 h2 .. + 7 of its row
     {
         const bf16_t *src = (const bf16_t *)a.q + (int64_t)(rq.row0 + tok) * a.q_stride + (int64_t)head * HD + 8 * h2;
@@ -79,176 +77,196 @@ __global__ __launch_bounds__(64 * prompt_waves(HD), HD == 256 ? 1 : 2) void k_pa
     }
 
     // ---- holes in the part of the table that this workgroup reads: then every block is looked at
-    const auto real = [&](int v) { return v < st.n_pre ? v : v + st.skip; };
     bool hole = false;
     if (s_begin < s_end) {
         const int p0 = (real(s_begin) * BLOCK) >> a.page_shift, p1 = (min((real(s_end - 1) + 1) * BLOCK, rq.n_keys) - 1) >> a.page_shift;
-        for (int p = p0 + tid; p <= p1; p += 64 * NWV) hole |= (unsigned)table[p] >= (unsigned)a.n_pages;
+        for (int p = p0 + tid; p <= p1; p += 64 * NWV) hole |= (unsigned)a.block_table[(int64_t)b * a.max_pages + p] >= (unsigned)a.n_pages;
     }
     hole = __syncthreads_or(hole);
 
-    // ---- fetching: this wave's positions of a block
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds;
+    // ---- fetching: every wave fetches sixteen positions of a block, which lie in one page, of both pools.  Chunk c of key row r
+    //      lies at chunk c ^ swizzle(r) in LDS, the values as they lie in the pool
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * 16 * HD * 2;
     constexpr int SWZ_SHIFT = CPR == 4 ? 2 : CPR == 8 ? 1 : 0, SWZ_MASK = CPR == 32 ? 15 : CPR - 1;
-    uint32_t koff[PIECES];
+    uint32_t koff[LOADS];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int r = i * (512 / HD) + lane / CPR, row = wave * KW + r;
-        koff[i] = r * HD * 2 + ((lane % CPR) ^ ((row >> SWZ_SHIFT) & SWZ_MASK)) * 16;
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = i * (512 / HD) + lane / CPR;
+        koff[i] = r * HD * 2 + ((lane % CPR) ^ ((r >> SWZ_SHIFT) & SWZ_MASK)) * 16;
     }
-    const auto page_of = [&](int step) {   // page number and offset of this wave's positions (elements)
-        const int key = step * BLOCK + wave * KW;
+    const auto place = [&](int step) {   // elements from a pool's start to this wave's positions
+        const int key = step * BLOCK + 16 * wave;
         const int id = table[min(key >> a.page_shift, a.max_pages - 1)];
         return (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (((int64_t)g << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * HD;
     };
-    const auto fetch = [&](int64_t at, int buf) {
-        if (KW * NWV > BLOCK && wave * KW >= BLOCK) return;
-        const bf16_t *kb = (const bf16_t *)a.k_pages + at, *vb = (const bf16_t *)a.v_pages + at;
-        const uint32_t dst = lds0 + buf * BUF + wave * KW * HD * 2;
+    const auto fetch = [&](int64_t at, int stage) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + stage * BUF;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) page_to_lds(dst + i * 1024, koff[i], kb);
+        for (int i = 0; i < LOADS; ++i) page_to_lds(to + i * 1024, koff[i], (const bf16_t *)a.k_pages + at);
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) page_to_lds(dst + HALF + i * 1024, i * 1024 + lane * 16, vb);
+        for (int i = 0; i < LOADS; ++i) page_to_lds(to + HALF + i * 1024, i * 1024 + lane * 16, (const bf16_t *)a.v_pages + at);
     };
 
     // ---- reading: K rows with bits 2 and 3 swapped, chunk 2 t + h2; V groups 2 kc + h2
     const int krow = (qi & ~12) | ((qi & 4) << 1) | ((qi & 8) >> 1);
-    uint32_t kaddr[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) kaddr[t] = krow * HD * 2 + (((2 * t + h2) ^ ((krow >> SWZ_SHIFT) & SWZ_MASK)) * 16);
+    const uint32_t kaddr = krow * HD * 2 + ((h2 ^ ((krow >> SWZ_SHIFT) & SWZ_MASK)) * 16);   // of chunk h2; chunk 2 t + h2 lies at kaddr ^ 32 t
     const uint32_t vaddr = HALF + (h2 * HD + qi) * 16;
 
-    const auto see_all = [&](int key0) {   // every row of the wave sees every key of the block
+    // every row from position p0 to p1 sees every key of the block
+    const auto see_all = [&](int key0, int p0, int p1) {
         return !hole && key0 + BLOCK <= rq.n_keys &&
-               (key0 + BLOCK <= rq.prefix || (key0 + BLOCK - 1 <= pos_min && (!a.window || key0 > pos_max - a.window)));
+               (key0 + BLOCK <= rq.prefix || (key0 + BLOCK - 1 <= p0 && (!a.window || key0 > p1 - a.window)));
     };
-    uint32_t odd = 0;   // bits of values that are not finite, of blocks that not every row sees
-    float m_ref = -INFINITY, l_run = 0.f;
+    const auto see_none = [&](int key0) {   // no row of the wave sees any
+        return !busy || (key0 >= rq.prefix && (key0 > pos_max || (a.window && key0 + BLOCK - 1 <= pos_min - a.window)));
+    };
+    const auto runs_there = [&](int key0) {   // bit i: run i of sixteen keys is in a page
+        uint32_t ok = 15;
+        if (hole) {
+            ok = 0;
+            for (int i = 0; i < 4; ++i) {
+                const int key = key0 + 16 * i;
+                if (key < rq.n_keys && (unsigned)table[key >> a.page_shift] < (unsigned)a.n_pages) ok |= 1u << i;
+            }
+        }
+        return ok;
+    };
+
+    int odd = 0;   // whether a value was not finite, of the blocks that not every row of the workgroup sees
+    float m_ref = -INFINITY, l_run[2] = {0.f, 0.f};
     paged_f16 o[OT];
 #pragma unroll
     for (int dt = 0; dt < OT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-    const float c = a.scale * 1.4426950408889634f;   // scores in units of ln 2
+    const float scale2 = a.scale * LOG2E;                                                   // scores in units of ln 2
+    const float cap_in = 2.f * scale2 / a.softcap, cap_out = a.softcap * LOG2E;             // (CAP only)
+    const paged_f16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-    int64_t next_at = 0;
+    int64_t at_next = 0;   // where this wave's positions of the next block to be fetched lie
     if (s_begin < s_end) {
-        fetch(page_of(real(s_begin)), 0);
-        next_at = page_of(real(min(s_begin + 1, s_end - 1)));
+        int64_t at[STAGES - 1];
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) at[i] = place(real(min(s_begin + i, s_end - 1)));
+        at_next = place(real(min(s_begin + STAGES - 1, s_end - 1)));
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (s_begin + i < s_end) fetch(at[i], i);
     }
     for (int s = s_begin; s < s_end; ++s) {
-        const int buf = (s - s_begin) & 1;
-        // this wave's part of block s has arrived, and so has everybody's; nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < s_end) {
-            fetch(next_at, buf ^ 1);
-            next_at = page_of(real(min(s + 2, s_end - 1)));
+        // block s has arrived, everybody's part of it, and nobody reads block s - 1 any more; its place takes block s - 1 + STAGES
+        constexpr int MOST = STAGES - 2, SOME = MOST / 3;   // blocks that may still be on their way, where there are so many
+        const int left = s_end - s - 1;
+        if (left >= MOST) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(MOST * WAITS) : "memory");
+        else if (left >= SOME) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SOME * WAITS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int stage = (s - s_begin) % STAGES, key0 = real(s) * BLOCK;
+        if (s + STAGES - 1 < s_end) {
+            fetch(at_next, (stage + STAGES - 1) % STAGES);
+            at_next = place(real(min(s + STAGES, s_end - 1)));
         }
-        const int key0 = real(s) * BLOCK;
-        const bool none = !busy || (key0 >= rq.prefix && (key0 > pos_max || (a.window && key0 + BLOCK - 1 <= pos_min - a.window)));
-        if (none) continue;
-        const bool whole = see_all(key0);
-        const unsigned char *kb = lds + buf * BUF;
+        if (!see_all(key0, tile_min, tile_max)) {
+            // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN would reach every row.
+            // The same holds for values that only some rows see: those that are not finite are taken out and added at the end.
+            const uint32_t ok = runs_there(key0);
+            uint32_t out = 0;
+            for (int i = tid; i < BLOCK * HD / 8; i += 64 * NWV) {
+                const int group = i / HD, n = ok >> (group >> 1) & 1 ? rq.n_keys - (key0 + 8 * group) : 0;   // of the group's eight keys
+                paged_u4 *to = reinterpret_cast<paged_u4 *>(lds + stage * BUF + HALF) + i;
+                paged_u4 v = *to;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    v[w] &= (2 * w < n ? 0xffffu : 0u) | (2 * w + 1 < n ? 0xffff0000u : 0u);
+                    const uint32_t fine = finite_halves(v[w]);
+                    out |= v[w] & ~fine;
+                    v[w] &= fine;
+                }
+                *to = v;
+            }
+            odd |= __syncthreads_or(out != 0);
+        }
+        if (see_none(key0)) continue;
+        // ---- scores: register r of tile i is key 32 i + 16 (r / 8) + 8 h2 + r % 8
         paged_f16 x[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[i][r] = 0.f;
-#pragma unroll
-            for (int t = 0; t < QT; ++t) x[i] = mfma32(*reinterpret_cast<const paged_u4 *>(kb + kaddr[t] + i * 32 * HD * 2), q[t], x[i]);
-        }
-        // register r of tile i: key key0 + 32 i + 16 (r / 8) + 8 h2 + r % 8
-        if (MODS) {
+            for (int i = 0; i < 2; ++i)
+                x[i] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + ((kaddr + stage * BUF) ^ (32 * t)) + i * 32 * HD * 2), q[t], t ? x[i] : zero);
+        if (MODS != PLAIN) {   // into units of ln 2, with cap and bias (PLAIN scales them with the exponentials)
+            const float near = slope * (float)(key0 + 8 * h2 - pos);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    float v = x[i][r] * a.scale;
-                    if (a.softcap > 0.f) v = a.softcap * paged_tanh_fast(v / a.softcap);
-                    if (a.slopes) v = fmaf(slope, (float)(key0 + 32 * i + 16 * (r >> 3) + 8 * h2 + (r & 7) - pos), v);
-                    x[i][r] = v * 1.4426950408889634f;
+                    const float bias = MODS & BIAS ? fmaf(slope, (float)(32 * i + 16 * (r >> 3) + (r & 7)), near) : 0.f;
+                    if (MODS & CAP) {
+                        const float t = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[i][r] * cap_in) + 1.f);   // tanh = 1 - 2 t
+                        x[i][r] = fmaf(t, -2.f * cap_out, cap_out + bias);
+                    } else {
+                        x[i][r] = fmaf(x[i][r], scale2, bias);
+                    }
                 }
         }
-        uint32_t run_ok = 15;   // bit i: run i of sixteen keys is in a page
-        if (!whole) {
-            if (hole) {
-                run_ok = 0;
-                for (int i = 0; i < 4; ++i) {
-                    const int key = key0 + 16 * i;
-                    if (key < rq.n_keys && (unsigned)table[key >> a.page_shift] < (unsigned)a.n_pages) run_ok |= 1u << i;
-                }
-            }
+        if (!see_all(key0, pos_min, pos_max)) {
+            const uint32_t ok = runs_there(key0);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int run = 2 * i + (r >> 3), j = key0 + 16 * run + 8 * h2 + (r & 7);
-                    x[i][r] = paged_sees(j, run_ok >> run & 1 ? rq.n_keys : 0, rq.prefix, pos, lo) ? x[i][r] : -INFINITY;
+                    x[i][r] = paged_sees(j, ok >> run & 1 ? rq.n_keys : 0, rq.prefix, pos, lo) ? x[i][r] : -INFINITY;
                 }
         }
+        // (the maximum that lets NaN through is one instruction for two values; a row with one is NaN whatever the reference)
         float mx = x[0][0];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[i][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        if (!MODS) mx *= c;
+            for (int r = 0; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, x[i][r]);
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
+        if (MODS == PLAIN) mx *= scale2;
         if (__any(mx > m_ref + 8.f)) {
             const float m_new = fmaxf(m_ref, mx);
             const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
             m_ref = m_new;
-            l_run *= alpha;
+            l_run[0] *= alpha;
+            l_run[1] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < OT; ++dt) o[dt] *= alpha;
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;   // a row that has seen no key yet
-        float sum[2] = {0.f, 0.f};
         paged_u4 p[4];
+        const auto probs = [&](int kc) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(MODS ? x[i][r] - sub : fmaf(x[i][r], c, -sub));
-                const float e1 = __builtin_amdgcn_exp2f(MODS ? x[i][r + 1] - sub : fmaf(x[i][r + 1], c, -sub));
-                sum[0] += e0;
-                sum[1] += e1;
-                p[2 * i + (r >> 3)][(r & 7) >> 1] = f32x2_to_bf16x2(e0, e1);
+            for (int w = 0; w < 4; ++w) {
+                const float x0 = x[kc >> 1][8 * (kc & 1) + 2 * w], x1 = x[kc >> 1][8 * (kc & 1) + 2 * w + 1];
+                const float e0 = __builtin_amdgcn_exp2f(MODS ? x0 - sub : fmaf(x0, scale2, -sub)), e1 = __builtin_amdgcn_exp2f(MODS ? x1 - sub : fmaf(x1, scale2, -sub));
+                l_run[0] += e0;
+                l_run[1] += e1;
+                p[kc][w] = f32x2_to_bf16x2(e0, e1);
             }
-        l_run += sum[0] + sum[1];
-        const unsigned char *vb = kb + vaddr;
-        if (whole) {
-#pragma unroll
-            for (int kc = 0; kc < 4; ++kc)
-#pragma unroll
-                for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(vb + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
-            continue;
-        }
-        // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN would reach every row.
-        // The same holds for values that only some rows see: those that are not finite are taken out here and added below.
+        };
+        // a run of sixteen keys' products, and the next run's exponentials beside them; the other workgroup's wave yields
+        probs(0);
+        __builtin_amdgcn_s_setprio(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kc = 0; kc < 4; ++kc) {
-            const int n = run_ok >> kc & 1 ? rq.n_keys - (key0 + 16 * kc + 8 * h2) : 0;   // of this lane's eight keys
 #pragma unroll
-            for (int dt = 0; dt < OT; ++dt) {
-                paged_u4 v = *reinterpret_cast<const paged_u4 *>(vb + (2 * kc * HD + 32 * dt) * 16);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    v[w] &= (2 * w < n ? 0xffffu : 0u) | (2 * w + 1 < n ? 0xffff0000u : 0u);
-                    const uint32_t fine = finite_halves(v[w]);
-                    odd |= v[w] & ~fine;
-                    v[w] &= fine;
-                }
-                o[dt] = mfma32(v, p[kc], o[dt]);
-            }
+            for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
+            if (kc < 3) probs(kc + 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
     }
 
-    if (__any(odd != 0)) {
-        // rare: some value of a block that not every row sees is not finite.  Each row takes those that it sees, by their kind
+    if (odd) {
+        // rare: a value that is not finite has been taken out.  Each row adds those that it sees (a second time where it has: they
+        // stay what they are)
 #pragma unroll 1
         for (int s = s_begin; s < s_end; ++s) {
             const int key0 = real(s) * BLOCK;
-            if (see_all(key0)) continue;
 #pragma unroll 1
             for (int j = key0; j < min(key0 + BLOCK, rq.n_keys); ++j) {
                 const int id = table[j >> a.page_shift], in = j & ((1 << a.page_shift) - 1);
@@ -261,8 +279,10 @@ __global__ __launch_bounds__(64 * prompt_waves(HD), HD == 256 ? 1 : 2) void k_pa
             }
         }
     }
+
+    float l = l_run[0] + l_run[1];
+    l += __shfl_xor(l, 32, 64);
     if (wrow + qi >= R) return;
-    const float l = l_run + __shfl_xor(l_run, 32, 64);
     const int64_t row = rq.row0 + tok;
     if (a.n_splits == 1) {
         const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees no key is 0
@@ -274,25 +294,24 @@ __global__ __launch_bounds__(64 * prompt_waves(HD), HD == 256 ? 1 : 2) void k_pa
                 *reinterpret_cast<uint2 *>(dst + 32 * dt + 8 * i) = make_uint2(f32x2_to_bf16x2(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
                                                                                 f32x2_to_bf16x2(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
     } else {
-        const int64_t at = ((int64_t)split * a.n_tokens + row) * a.H + head;
+        const int64_t to = ((int64_t)split * a.n_tokens + row) * a.H + head;
         if (l != 0.f) {   // (a part without keys is not read)
 #pragma unroll
             for (int dt = 0; dt < OT; ++dt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<paged_f4 *>(a.po + at * HD + 32 * dt + 8 * i + 4 * h2) = paged_f4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+                    *reinterpret_cast<paged_f4 *>(a.po + to * HD + 32 * dt + 8 * i + 4 * h2) = paged_f4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
         }
         if (h2 == 0) {
-            a.pm[at] = m_ref;
-            a.pl[at] = l;
+            a.pm[to] = m_ref;
+            a.pl[to] = l;
         }
     }
 }
 
-int paged_prompt_rows(int head_dim) { return 32 * prompt_waves(head_dim); }
-int paged_prompt_tiles(const PagedAttn &a, int head_dim) { return (int)((int64_t)a.n_tokens * a.rep / paged_prompt_rows(head_dim)) + a.batch; }
+int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
-template <int HD, bool MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
+template <int HD, int MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
     static bool allowed[MAX_DEVICES];
     const size_t lds = prompt_lds(HD);
     if (lds > 60 * 1024 && !(device >= 0 && device < MAX_DEVICES && allowed[device])) {
@@ -302,17 +321,21 @@ template <int HD, bool MODS> static const char *launch_t(const PagedAttn &a, int
         }
         if (device >= 0 && device < MAX_DEVICES) allowed[device] = true;
     }
-    hipLaunchKernelGGL((k_paged_prompt<HD, MODS>), dim3(paged_prompt_tiles(a, HD) * a.G, a.n_splits), dim3(64 * prompt_waves(HD)), lds, stream, a);
+    hipLaunchKernelGGL((k_paged_prompt<HD, MODS>), dim3(paged_prompt_tiles(a) * a.G, a.n_splits), dim3(64 * PROMPT_WAVES), lds, stream, a);
     return nullptr;
 }
+template <int HD> static const char *launch_m(const PagedAttn &a, int device, hipStream_t stream) {
+    const bool cap = a.softcap > 0.f;
+    // (PLAIN scales the maximum in the place of the scores, which only a positive scale keeps a maximum)
+    if (a.slopes || (a.scale < 0.f && !cap)) return cap ? launch_t<HD, CAP | BIAS>(a, device, stream) : launch_t<HD, BIAS>(a, device, stream);
+    return cap ? launch_t<HD, CAP>(a, device, stream) : launch_t<HD, PLAIN>(a, device, stream);
+}
 const char *launch_paged_prompt(const PagedAttn &a, int head_dim, int device, hipStream_t stream) {
-    // (without cap and bias the scale is applied to the maximum, which only a positive one keeps a maximum)
-    const bool mods = a.softcap > 0.f || a.slopes || a.scale < 0.f;
     switch (head_dim) {
-        case 32: return mods ? launch_t<32, true>(a, device, stream) : launch_t<32, false>(a, device, stream);
-        case 64: return mods ? launch_t<64, true>(a, device, stream) : launch_t<64, false>(a, device, stream);
-        case 128: return mods ? launch_t<128, true>(a, device, stream) : launch_t<128, false>(a, device, stream);
-        default: return mods ? launch_t<256, true>(a, device, stream) : launch_t<256, false>(a, device, stream);
+        case 32: return launch_m<32>(a, device, stream);
+        case 64: return launch_m<64>(a, device, stream);
+        case 128: return launch_m<128>(a, device, stream);
+        default: return launch_m<256>(a, device, stream);
     }
 }
 

@@ -39,13 +39,12 @@ constexpr int PAGED_MAX_SPLITS = 64;   // the kernel that joins them gives each 
 // What a call will launch, from the sizes and the hints alone
 struct PagedCut {
     bool rows, prompt;             // k_paged_rows, k_paged_prompt (both: requests go by row_limit)
-    int n_splits;
+    int n_splits, split_steps;     // split_steps: of 64 keys
     size_t workspace;              // bytes
 };
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len);
-// The kernel of many rows (bf16): its rows per tile and how many tiles a call has at most
-int paged_prompt_rows(int head_dim);
-int paged_prompt_tiles(const PagedAttn &a, int head_dim);
+// The kernel of many rows (bf16), and how many tiles a call has at most
+int paged_prompt_tiles(const PagedAttn &a);
 const char *launch_paged_prompt(const PagedAttn &a, int head_dim, int device, hipStream_t stream);
 // null, or why the launch failed
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream);
@@ -74,6 +73,20 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedAttn &a, int b)
     r.n_keys = min((int64_t)len, (int64_t)a.max_pages << a.page_shift);
     r.prefix = min(max(pre, 0), r.n_keys);
     return r;
+}
+
+// Ragged tiles: request b owns the tiles from floor(q_start[b] rep / rows) + b on, at least as many as it needs.  The request
+// that owns `tile`, found by a wave: 64 candidates at a time.
+__device__ __forceinline__ int paged_find(const PagedAttn &a, int tile, int rows, int lane) {
+    int b = 0;
+    for (int n = a.batch; n > 1;) {
+        const int stride = (n + 63) / 64, at = lane * stride;
+        const bool before = at < n && (int64_t)min(max(a.q_start[b + min(at, n - 1)], 0), a.n_tokens) * a.rep / rows + b + at <= tile;
+        const int k = max(__popcll(__ballot(before)) - 1, 0);
+        b = __builtin_amdgcn_readfirstlane(b + k * stride);
+        n = __builtin_amdgcn_readfirstlane(min(stride, n - k * stride));
+    }
+    return b;
 }
 
 // The key steps some row of a tile sees: the prefix's, then from the window of its first row to its last position.
