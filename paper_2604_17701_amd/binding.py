@@ -372,9 +372,10 @@ class Context:
         return self.wisv_ss_decide(*args, entry="wisv_ss_decide_static", **kw)
 
     # ---------------------------------------------------------------- paged cache
-    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them.
+    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them.  A server makes
+    # them once per layer and step: tensors in the usual layout are accepted by a few comparisons, the others by the helpers.
     def _stream_now(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream or _NULL_STREAM
+        return torch._C._cuda_getCurrentRawStream(self.device.index) or _NULL_STREAM
 
     def _ints(self, name: str, t: torch.Tensor, shape) -> int:
         if t.dtype is not torch.int32 or t.device != self.device or t.shape != shape or not t.is_contiguous():
@@ -391,23 +392,24 @@ class Context:
         if t.dim() != 3 or t.dtype is not dtype or t.device != self.device or t.shape[0] != rows or t.shape[2] != head_dim:
             raise ValueError(f"{name} must be [{rows}, heads, {head_dim}] of {dtype} on {self.device}")
         heads, (s0, s1, s2) = t.shape[1], t.stride()
-        if t.numel() and (s2 != 1 or (heads > 1 and s1 != head_dim)):
+        if (s2 != 1 or (heads > 1 and s1 != head_dim)) and t.numel():
             raise ValueError(f"the heads of a row of {name} must lie close together")
         return t.data_ptr(), heads, s0 if rows > 1 else heads * head_dim
 
     def _pools(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         """(pages, KV heads, page size, head_dim, wisv_dtype, page stride) of a pair of pools."""
-        dt = k_pages.dtype
-        if dt not in (torch.bfloat16, torch.float32) or v_pages.dtype is not dt or k_pages.device != self.device \
-                or v_pages.device != self.device or k_pages.dim() != 4:
-            raise ValueError(f"the pools must be bfloat16 or float32 tensors on {self.device}, of one type")
+        dt, dev = k_pages.dtype, self.device
+        if (dt is not torch.bfloat16 and dt is not torch.float32) or v_pages.dtype is not dt or k_pages.device != dev \
+                or v_pages.device != dev or k_pages.dim() != 4:
+            raise ValueError(f"the pools must be bfloat16 or float32 tensors on {dev}, of one type")
         n, g, ps, hd = k_pages.shape
-        if ps % 8 or v_pages.shape != (n, g, ps // 8, hd, 8):
+        if ps & 7 or v_pages.shape != (n, g, ps >> 3, hd, 8):
             raise ValueError("the pools must be [pages, kv heads, page size, head_dim] and [pages, kv heads, page size / 8, head_dim, 8]")
-        stride = k_pages.stride(0) if n > 1 else g * ps * hd
+        stride = g * ps * hd
         if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
-            close = (v_pages.stride(0) if n > 1 else stride) == stride and k_pages[:1].is_contiguous() and v_pages[:1].is_contiguous()
-            if not close:
+            if n > 1:
+                stride = k_pages.stride(0)
+            if (n > 1 and v_pages.stride(0) != stride) or not (k_pages[:1].is_contiguous() and v_pages[:1].is_contiguous()):
                 raise ValueError("a page must lie in one piece, and both pools must have the same distance from page to page")
         return n, g, ps, hd, WISV_BF16 if dt is torch.bfloat16 else WISV_F32, stride
 
@@ -415,22 +417,30 @@ class Context:
                         block_table: torch.Tensor, page_size: int, max_tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
         """Plans a step: cached_len, new_len int32 [batch], free_pages int32 [n_free], block_table int32 [batch, max_pages]
         (updated in place).  `out`: the tensors of an earlier plan of the same sizes, to be written again."""
-        b = cached_len.numel()
-        if out is None:
-            if max_tokens < 1:
-                raise ValueError("max_tokens must be positive")
-            sizes = (b + 1, b, max_tokens, max_tokens, 1, b)
-            out = PagePlan(*torch.empty(sum(sizes), dtype=torch.int32, device=self.device).split(sizes))
-            ptrs = [t.data_ptr() for t in out]
-        else:
-            ptrs = [self._ints(n, t, (m,)) for n, t, m in zip(PagePlan._fields, out, (b + 1, b, max_tokens, max_tokens, 1, b))]
+        b, n_free = cached_len.numel(), free_pages.numel()
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
-        width, n_free = block_table.shape[1], free_pages.numel()
+        width = block_table.shape[1]
+        if max_tokens < 1:
+            raise ValueError("max_tokens must be positive")
+        sizes = (b + 1, b, max_tokens, max_tokens, 1, b)
+        if out is None:
+            buf = torch.empty(3 * b + 2 + 2 * max_tokens, dtype=torch.int32, device=self.device)
+            out = PagePlan._make(buf.split(sizes))
+            p = buf.data_ptr()
+            kv = p + 4 * b + 4
+            pos = kv + 4 * b
+            slots = pos + 4 * max_tokens
+            used = slots + 4 * max_tokens
+            ptrs = (p, kv, pos, slots, used, used + 4)
+        else:
+            ptrs = [self._ints(n, t, (m,)) for n, t, m in zip(PagePlan._fields, out, sizes)]
         args = wisv_paged_plan_args(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, (b,)),
                                     self._ints("new_len", new_len, (b,)), self._ints("free_pages", free_pages, (n_free,)) or None,
                                     self._ints("block_table", block_table, (b, width)), *ptrs, self._stream_now())
-        self._check(self._lib.wisv_paged_plan(self._h, C.byref(args)))
+        rc = self._lib.wisv_paged_plan(self._h, C.byref(args))
+        if rc:
+            self._check(rc)
         return out
 
     def wisv_paged_append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
@@ -445,27 +455,32 @@ class Context:
         vp, vg, vs = self._rows("v", v, dt, rows, hd)
         if kg != g or vg != g:
             raise ValueError(f"k and v must have the pools' {g} heads")
-        qp = qop = None
-        heads = qs = qos = 0
+        qp = qop = pp = cp = sp = None
+        heads = qs = qos = n_rope = 0
         if q is not None:
             qp, heads, qs = self._rows("q", q, dt, rows, hd)
             if q_out is None:
                 q_out = torch.empty((rows, heads, hd), dtype=dt, device=self.device)
-            qop, oh, qos = self._rows("q_out", q_out, dt, rows, hd)
-            if oh != heads:
-                raise ValueError("q_out must have the heads of q")
+                qop, qos = q_out.data_ptr(), heads * hd
+            else:
+                qop, oh, qos = self._rows("q_out", q_out, dt, rows, hd)
+                if oh != heads:
+                    raise ValueError("q_out must have the heads of q")
         elif q_out is not None:
             raise ValueError("q_out without q")
-        if (cos is None) != (sin is None) or (cos is not None and (positions is None or cos.dim() != 2)):
-            raise ValueError("cos and sin come together, [n_rope, head_dim / 2], and need positions")
-        n_rope = 0 if cos is None else cos.shape[0]
-        args = wisv_paged_append_args(
-            rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos,
-            None if positions is None else self._ints("positions", positions, (rows,)), self._ints("slots", slots, (rows,)),
-            None if cos is None else self._floats("cos", cos, (n_rope, hd // 2)),
-            None if sin is None else self._floats("sin", sin, (n_rope, hd // 2)), k_pages.data_ptr(), v_pages.data_ptr(), stride,
-            self._stream_now())
-        self._check(self._lib.wisv_paged_append(self._h, C.byref(args)))
+        if positions is not None:
+            pp = self._ints("positions", positions, (rows,))
+        if cos is not None or sin is not None:
+            if cos is None or sin is None or pp is None or cos.dim() != 2:
+                raise ValueError("cos and sin come together, [n_rope, head_dim / 2], and need positions")
+            n_rope = cos.shape[0]
+            cp, sp = self._floats("cos", cos, (n_rope, hd >> 1)), self._floats("sin", sin, (n_rope, hd >> 1))
+        args = wisv_paged_append_args(rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos, pp,
+                                      self._ints("slots", slots, (rows,)), cp, sp, k_pages.data_ptr(), v_pages.data_ptr(), stride,
+                                      self._stream_now())
+        rc = self._lib.wisv_paged_append(self._h, C.byref(args))
+        if rc:
+            self._check(rc)
         return q_out
 
     def wisv_paged_attention(self, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
@@ -482,29 +497,36 @@ class Context:
         rows, dt = q.shape[0], k_pages.dtype
         qp, heads, qs = self._rows("q", q, dt, rows, hd)
         if out is None:
-            out = torch.empty((rows, heads, hd), dtype=dt, device=self.device)
-        op, oh, os_ = self._rows("out", out, dt, rows, hd)
-        if oh != heads:
-            raise ValueError("out must have the heads of q")
-        b = kv_len.numel()
+            out = torch.empty_like(q) if qs == heads * hd else torch.empty((rows, heads, hd), dtype=dt, device=self.device)
+            op, os_ = out.data_ptr(), heads * hd
+        else:
+            op, oh, os_ = self._rows("out", out, dt, rows, hd)
+            if oh != heads:
+                raise ValueError("out must have the heads of q")
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
+        b, width = kv_len.numel(), block_table.shape[1]
         args = wisv_paged_attention_args(
-            b, rows, heads, g, hd, dtype, ps, n, block_table.shape[1], max_new, max_len, window, scale, softcap, qp, op, qs, os_,
-            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, (b, block_table.shape[1])),
+            b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,
+            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, (b, width)),
             self._ints("q_start", q_start, (b + 1,)), self._ints("kv_len", kv_len, (b,)),
             None if prefix_len is None else self._ints("prefix_len", prefix_len, (b,)),
             None if slopes is None else self._floats("slopes", slopes, (heads,)), None, 0, self._stream_now())
+        ref = C.byref(args)
         if workspace is None:
             need = C.c_size_t()
-            self._check(self._lib.wisv_paged_attention_workspace(self._h, C.byref(args), C.byref(need)))
+            rc = self._lib.wisv_paged_attention_workspace(self._h, ref, C.byref(need))
+            if rc:
+                self._check(rc)
             if need.value:
                 workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
         elif workspace.device != self.device or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {self.device}")
         if workspace is not None:
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        self._check(self._lib.wisv_paged_attention(self._h, C.byref(args)))
+        rc = self._lib.wisv_paged_attention(self._h, ref)
+        if rc:
+            self._check(rc)
         return out
 
     # ---------------------------------------------------------------- state

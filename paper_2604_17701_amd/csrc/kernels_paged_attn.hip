@@ -32,11 +32,11 @@ struct StepPages {
     bool has[2];
 };
 template <typename T, int HD>
-__device__ __forceinline__ StepPages step_pages(const PagedAttn &a, const int32_t *row, int g, int step) {
+__device__ __forceinline__ StepPages step_pages(const PagedAttn &a, paged_ints row, int g, int step) {
     constexpr int KEYS = Step<T>::KEYS;
     const int key = step * KEYS, p0 = key >> a.page_shift;
     StepPages s;
-    const int id0 = row[p0], in = key & ((1 << a.page_shift) - 1);
+    const int id0 = row[min(p0, a.max_pages - 1)], in = key & ((1 << a.page_shift) - 1);
     const bool ok0 = (unsigned)id0 < (unsigned)a.n_pages;
     s.has[0] = ok0;
     s.at[0] = (int64_t)(ok0 ? id0 : 0) * a.page_stride + (((int64_t)g << a.page_shift) + in) * HD;
@@ -51,7 +51,8 @@ __device__ __forceinline__ StepPages step_pages(const PagedAttn &a, const int32_
     return s;
 }
 
-constexpr int NW = 4;   // waves of a workgroup of k_paged_rows
+// Waves of a workgroup of k_paged_rows: eight, two to a SIMD, where the registers of half a SIMD hold a wave, else four
+constexpr int rows_waves(int hd, int nq) { return hd * nq <= 128 ? 8 : 4; }
 
 constexpr int merge_tiles(int nw, int nq, int dt) {   // feature tiles of 16 joined at a time: at most 32 KB of LDS
     int d = dt;
@@ -60,7 +61,8 @@ constexpr int merge_tiles(int nw, int nq, int dt) {   // feature tiles of 16 joi
 }
 
 template <typename T, int HD, int NQ, bool MODS>
-__global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
+__global__ __launch_bounds__(64 * rows_waves(HD, NQ)) void k_paged_rows(PagedAttn a) {
+    constexpr int NW = rows_waves(HD, NQ);
     constexpr int KEYS = Step<T>::KEYS, E = Step<T>::E, KL = HD / 16, QL = HD * (int)sizeof(T) / 64, DT = HD / 16;
     constexpr int DP = merge_tiles(NW, NQ, DT);
     constexpr bool BF = sizeof(T) == 2;
@@ -68,19 +70,27 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
     __shared__ paged_f4 so[NW][NQ][DP][64];
     const int tid = threadIdx.x, lane = tid & 63, bj = lane & 15, bg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = blockIdx.x % a.G, b = blockIdx.x / a.G, split = blockIdx.y;
+    const int g = blockIdx.x % a.G, split = blockIdx.y;
+    // a workgroup per request, or (tiles) per tile
+    const PagedTile mine = a.tiles ? paged_find(a, blockIdx.x / a.G, 16 * NQ, lane) : PagedTile{(int)blockIdx.x / a.G, 0};
+    if (mine.b < 0) return;
+    const int b = mine.b;
+    const paged_ints table = (paged_ints)(uintptr_t)(a.block_table + (int64_t)b * a.max_pages);
+    // the pages of the step that is this wave's first unless a window or a prefix says otherwise: asked for beside the lengths
+    const int guess = split * a.split_steps + wave;
+    const StepPages guessed = step_pages<T, HD>(a, table, g, guess);
     const PagedRequest rq = paged_request(a, b);
     const int R = rq.n_new * a.rep;
-    if (a.row_limit && R > a.row_limit) return;
-    const int32_t *table = a.block_table + (int64_t)b * a.max_pages;
     const T *kpool = (const T *)a.k_pages, *vpool = (const T *)a.v_pages;
+    constexpr float LOG2E = 1.4426950408889634f;
+    const float scale2 = a.scale * LOG2E, cap_out = a.softcap * LOG2E, cap_in = (BF ? 2.f * scale2 : a.scale) / a.softcap;   // (cap_in: only with a cap)
     // this lane's part of a step: keys of its K rows lie in run krun, those of its V operand and scores in run vrun
     constexpr int HALF = KEYS / 2;
     const int krow = BF ? 8 * ((bj >> 2) & 1) + (bj & 3) : bj & 7, krun = bj >> 3, vrun = bg >> 1;
     const int koff = krow * HD + (BF ? 8 : 4) * bg;
     const int voff = BF ? ((bg & 1) * HD + bj) * 8 : bj * 8 + (bg & 1) * 4;
 
-    for (int rho0 = 0; rho0 < R; rho0 += 16 * NQ) {
+    for (int rho0 = mine.index * 16 * NQ; rho0 < R; rho0 += a.tiles ? R : 16 * NQ) {
         const int rho_end = min(rho0 + 16 * NQ, R);
         const int pos_min = rq.pos0 + rho0 / a.rep, pos_max = rq.pos0 + (rho_end - 1) / a.rep;
         const PagedSteps st = paged_steps(rq, pos_min, pos_max, a.window, KEYS);
@@ -98,7 +108,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
 #pragma unroll
             for (int t = 0; t < QL; ++t) q[nq][t] = *reinterpret_cast<const paged_u4 *>(src + t * (BF ? 32 : 16));
             pos[nq] = rq.pos0 + tok;
-            slope[nq] = MODS && a.slopes ? a.slopes[h] : 0.f;
+            slope[nq] = MODS && a.slopes ? a.slopes[h] * LOG2E : 0.f;
         }
         float m_run[NQ], l_run[NQ];
         paged_f4 oacc[NQ][DT];
@@ -137,7 +147,7 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                        (key0 + KEYS <= rq.prefix || (key0 + KEYS - 1 <= pos_min && (!a.window || key0 > pos_max - a.window)));
             };
             uint32_t odd = 0;   // bits of values that are not finite, of steps that not every row sees
-            StepPages cur = step_pages<T, HD>(a, table, g, real(s));
+            StepPages cur = real(s) == guess ? guessed : step_pages<T, HD>(a, table, g, real(s));
             load_k(cur);
             load_v(cur);
             StepPages nxt = step_pages<T, HD>(a, table, g, real(min(s + NW, s_end - 1)));
@@ -168,12 +178,15 @@ __global__ __launch_bounds__(64 * NW) void k_paged_rows(PagedAttn a) {
                     float x[E];
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        float v = (e < 4 ? sa[e] : sb[e & 3]) * a.scale;
-                        if (MODS) {
-                            if (a.softcap > 0.f) v = a.softcap * (BF ? paged_tanh_fast(v / a.softcap) : tanhf(v / a.softcap));
-                            if (a.slopes) v = fmaf(slope[nq], (float)(kbase + e - pos[nq]), v);
+                        // in units of ln 2: every exponential is one instruction
+                        float v = e < 4 ? sa[e] : sb[e & 3];
+                        if (MODS && a.softcap > 0.f) {
+                            if (BF) v = fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v * cap_in) + 1.f), -2.f * cap_out, cap_out);   // tanh = 1 - 2 / (exp(2 x) + 1)
+                            else v = cap_out * tanhf(v * cap_in);
+                        } else {
+                            v *= scale2;
                         }
-                        x[e] = v * 1.4426950408889634f;   // in units of ln 2: every exponential is one instruction
+                        x[e] = MODS ? fmaf(slope[nq], (float)(kbase + e - pos[nq]), v) : v;
                     }
                     if (!whole) {
                         const int lo = a.window ? pos[nq] - a.window : -1;
@@ -407,13 +420,17 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
 
 // ------------------------------------------------------------------------------------------ launch
 
-// rows of a request that k_paged_rows reads the keys once for
-constexpr int ROW_LIMIT = 32;
+// Rows of a request that k_paged_rows takes: beyond them it would read the keys twice, and k_paged_prompt, which holds
+// 128, serves bf16.  At head_dim 128 that kernel is as fast from 17 rows on: 64 requests of 32 rows over 8192 positions 361 us, two
+// tiles of 16 here 370, 16 requests of 24 rows over 2048 30.1 and 30.7 (head_dim 64, 256 requests of 32 rows over 2048 235 and 205;
+// 256, 64 over 4096 446 and 390).
+static int row_limit(bool bf16, int head_dim) { return bf16 && head_dim == 128 ? 16 : 32; }
 
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len) {
     PagedCut c;
-    c.prompt = bf16 && (int64_t)a.rep * max_new > ROW_LIMIT;
-    c.rows = !c.prompt || a.batch > 1;
+    const int64_t rows = (int64_t)a.rep * max_new;
+    const bool many = rows > row_limit(bf16, head_dim);
+    c.prompt = bf16 && many;
     // positions that a tile's rows see at most: a window's are those of its first row and what its rows span
     const int reach = a.window ? (int)std::min<int64_t>(max_len, (int64_t)a.window + 64 + (c.prompt ? 128 / a.rep : max_new)) : max_len;
     const int64_t steps = (reach + 63) / 64;
@@ -430,8 +447,16 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     } else {
-        const int64_t wgs = std::max<int64_t>(1, (int64_t)a.batch * a.G);
-        c.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / wgs, (steps * 2 + NW - 1) / NW), PAGED_MAX_SPLITS));
+        // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 2.5 (its start and its
+        // end), the join and its launch 5 and the parts' way through memory
+        const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / 32, a.batch) : a.batch) * a.G;
+        const double unit = 128.0 * head_dim * (bf16 ? 2 : 4) / 36e3, part = (double)a.n_tokens * a.H * head_dim * 8 / 4e6;
+        double best = 0;
+        c.n_splits = 1;
+        for (int s = 1; s <= PAGED_MAX_SPLITS && (s == 1 || steps / s >= 2); ++s) {
+            const double cost = (double)((wgs * s + 255) / 256) * (unit * steps / s + 2.5) + (s > 1 ? 5 + s * part : 0);
+            if (s == 1 || cost < best) best = cost, c.n_splits = s;
+        }
     }
     c.split_steps = (int)((steps + c.n_splits - 1) / c.n_splits);
     c.workspace = c.n_splits == 1 ? 0 : (size_t)c.n_splits * a.n_tokens * a.H * (head_dim + 2) * 4;
@@ -439,20 +464,20 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
 }
 
 template <typename T, int HD, int NQ> static void launch_rows(const PagedAttn &a, hipStream_t stream) {
-    const dim3 grid(a.batch * a.G, a.n_splits);
-    if (a.softcap > 0.f || a.slopes) hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, true>), grid, dim3(64 * NW), 0, stream, a);
-    else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, false>), grid, dim3(64 * NW), 0, stream, a);
+    const dim3 grid((a.tiles ? (unsigned)((int64_t)a.n_tokens * a.rep / (16 * NQ) + a.batch) : a.batch) * a.G, a.n_splits);
+    if (a.softcap > 0.f || a.slopes) hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, true>), grid, dim3(64 * rows_waves(HD, NQ)), 0, stream, a);
+    else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, false>), grid, dim3(64 * rows_waves(HD, NQ)), 0, stream, a);
 }
-template <typename T, int HD> static void launch_rows_t(const PagedAttn &a, int rows, hipStream_t stream) {
-    if (rows <= 16) launch_rows<T, HD, 1>(a, stream);
-    else launch_rows<T, HD, 2>(a, stream);
+template <typename T, int HD> static void launch_rows_t(const PagedAttn &a, bool two, hipStream_t stream) {
+    if constexpr (sizeof(T) == 2 && HD == 128) return launch_rows<T, HD, 1>(a, stream);   // (row_limit)
+    else return two ? launch_rows<T, HD, 2>(a, stream) : launch_rows<T, HD, 1>(a, stream);
 }
-template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim, int rows, hipStream_t stream) {
+template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim, bool two, hipStream_t stream) {
     switch (head_dim) {
-        case 32: return launch_rows_t<T, 32>(a, rows, stream);
-        case 64: return launch_rows_t<T, 64>(a, rows, stream);
-        case 128: return launch_rows_t<T, 128>(a, rows, stream);
-        default: return launch_rows_t<T, 256>(a, rows, stream);
+        case 32: return launch_rows_t<T, 32>(a, two, stream);
+        case 64: return launch_rows_t<T, 64>(a, two, stream);
+        case 128: return launch_rows_t<T, 128>(a, two, stream);
+        default: return launch_rows_t<T, 256>(a, two, stream);
     }
 }
 template <typename T, int HD> static void launch_join_t(const PagedAttn &a, hipStream_t stream) {
@@ -473,16 +498,15 @@ template <typename T> static void launch_join(const PagedAttn &a, int head_dim, 
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream) {
     const PagedCut cut = paged_cut(a, bf16, head_dim, max_new, max_len);
     a.n_splits = cut.n_splits;
-    a.row_limit = cut.rows && cut.prompt ? ROW_LIMIT : 0;
     if (cut.prompt) {
         a.split_steps = cut.split_steps;
         if (const char *why = launch_paged_prompt(a, head_dim, device, stream)) return why;
-    }
-    if (cut.rows) {
+    } else {
         a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
-        const int rows = (int)std::min<int64_t>((int64_t)a.rep * max_new, ROW_LIMIT);
-        if (bf16) launch_rows_d<bf16_t>(a, head_dim, rows, stream);
-        else launch_rows_d<float>(a, head_dim, rows, stream);
+        const int64_t rows = (int64_t)a.rep * max_new;
+        a.tiles = rows > row_limit(bf16, head_dim);
+        if (bf16) launch_rows_d<bf16_t>(a, head_dim, rows > 16, stream);
+        else launch_rows_d<float>(a, head_dim, rows > 16, stream);
     }
     if (a.n_splits > 1) {
         if (bf16) launch_join<bf16_t>(a, head_dim, stream);

@@ -46,18 +46,15 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
     const int tid = threadIdx.x, lane = tid & 63, h2 = lane >> 5, qi = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = blockIdx.x % a.G, split = blockIdx.y;
-    const int tile = gridDim.x / a.G - 1 - blockIdx.x / a.G;   // later rows see more keys: they start first
-    const int b = paged_find(a, tile, ROWS, lane);
+    const PagedTile mine = paged_find(a, blockIdx.x / a.G, ROWS, lane);
+    if (mine.b < 0) return;
+    const int b = mine.b;
     const PagedRequest rq = paged_request(a, b);
     const int R = rq.n_new * a.rep;
-    const int64_t first = (int64_t)rq.row0 * a.rep / ROWS + b;
-    if (tile < first || (tile - first) * ROWS >= R || R <= a.row_limit) return;
-    const int rho0 = (int)(tile - first) * ROWS;
+    const int rho0 = ((R + ROWS - 1) / ROWS - 1 - mine.index) * ROWS;   // a request's later rows see more keys: they start first
     const PagedSteps st = paged_steps(rq, rq.pos0 + rho0 / a.rep, rq.pos0 + (min(rho0 + ROWS, R) - 1) / a.rep, a.window, BLOCK);
     const int s_begin = split * a.split_steps, s_end = split == a.n_splits - 1 ? st.total : min(st.total, s_begin + a.split_steps);
-    // (the table is read through the scalar cache: a vector load's wait would be one for the loads on their way to LDS)
-    typedef const int32_t __attribute__((address_space(4))) *const_ints;
-    const const_ints table = (const_ints)(uintptr_t)(a.block_table + (int64_t)b * a.max_pages);
+    const paged_ints table = (paged_ints)(uintptr_t)(a.block_table + (int64_t)b * a.max_pages);
     const auto real = [&](int v) { return v < st.n_pre ? v : v + st.skip; };
 
     const int tile_min = rq.pos0 + rho0 / a.rep, tile_max = rq.pos0 + (min(rho0 + ROWS, R) - 1) / a.rep;

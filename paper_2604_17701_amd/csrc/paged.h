@@ -26,7 +26,7 @@ void launch_paged_append(const PagedAppend &a, bool bf16, int head_dim, hipStrea
 struct PagedAttn {
     int batch, n_tokens, H, G, rep, n_pages, max_pages, page_shift, window;
     int n_splits, split_steps;     // key steps of a split; the last split takes what is left
-    int row_limit;                 // requests of more rows than this belong to the other kernel of the launch (0: none do)
+    bool tiles;                    // k_paged_rows: a workgroup per tile of rows and not per request
     float scale, softcap;
     const void *q, *k_pages, *v_pages;
     void *out;
@@ -38,7 +38,7 @@ struct PagedAttn {
 constexpr int PAGED_MAX_SPLITS = 64;   // the kernel that joins them gives each a lane
 // What a call will launch, from the sizes and the hints alone
 struct PagedCut {
-    bool rows, prompt;             // k_paged_rows, k_paged_prompt (both: requests go by row_limit)
+    bool prompt;                   // k_paged_prompt, or k_paged_rows
     int n_splits, split_steps;     // split_steps: of 64 keys
     size_t workspace;              // bytes
 };
@@ -54,6 +54,9 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
 typedef __bf16 paged_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float paged_f4 __attribute__((ext_vector_type(4)));
 typedef unsigned int paged_u4 __attribute__((ext_vector_type(4)));
+
+// tables read through the scalar cache (a vector load's wait would be one for the loads of keys and values as well)
+typedef const int32_t __attribute__((address_space(4))) *paged_ints;
 
 // What a workgroup knows of its request.  Every number is brought into the range the buffers have, whatever the arrays hold.
 struct PagedRequest {
@@ -75,18 +78,44 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedAttn &a, int b)
     return r;
 }
 
-// Ragged tiles: request b owns the tiles from floor(q_start[b] rep / rows) + b on, at least as many as it needs.  The request
-// that owns `tile`, found by a wave: 64 candidates at a time.
-__device__ __forceinline__ int paged_find(const PagedAttn &a, int tile, int rows, int lane) {
-    int b = 0;
-    for (int n = a.batch; n > 1;) {
-        const int stride = (n + 63) / 64, at = lane * stride;
-        const bool before = at < n && (int64_t)min(max(a.q_start[b + min(at, n - 1)], 0), a.n_tokens) * a.rep / rows + b + at <= tile;
-        const int k = max(__popcll(__ballot(before)) - 1, 0);
-        b = __builtin_amdgcn_readfirstlane(b + k * stride);
-        n = __builtin_amdgcn_readfirstlane(min(stride, n - k * stride));
+// Ragged tiles: request b owns ceil(its rows / rows) of them, one request behind the other, so that the workgroups without a tile
+// are the grid's last.  (Leaving gaps costs: with every second workgroup empty the dispatch gives some CUs three of the others and
+// some one, 64 requests of 128 rows over 8192 positions 533 us instead of 363.)  A wave finds the request that owns `tile`, 512
+// candidates at a time.
+struct PagedTile {
+    int b, index;   // the request, and which of its tiles; b < 0: there is no such tile
+};
+__device__ __forceinline__ PagedTile paged_find(const PagedAttn &a, int tile, int rows, int lane) {
+    constexpr int PER = 8;
+    int left = tile;
+    for (int b0 = 0; b0 < a.batch; b0 += 64 * PER) {
+        int start[PER + 1], count[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i <= PER; ++i) start[i] = min(max(a.q_start[min(b0 + lane * PER + i, a.batch)], 0), a.n_tokens);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            count[i] = max(start[i + 1] - start[i], 0);   // (past the last request: none)
+            count[i] = (int)(((int64_t)count[i] * a.rep + rows - 1) / rows);
+            sum += count[i];
+        }
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += y;
+        }
+        const unsigned long long beyond = __ballot(upto > left);
+        if (beyond) {
+            const int owner = __ffsll(beyond) - 1;
+            int in = left - (upto - sum), b = b0 + lane * PER;   // (of the owner's lane)
+#pragma unroll
+            for (int i = 0; i < PER - 1; ++i)
+                if (in >= count[i] && b == b0 + lane * PER + i) in -= count[i], ++b;
+            return PagedTile{__builtin_amdgcn_readfirstlane(__shfl(b, owner, 64)), __builtin_amdgcn_readfirstlane(__shfl(in, owner, 64))};
+        }
+        left -= __builtin_amdgcn_readfirstlane(__shfl(upto, 63, 64));
     }
-    return b;
+    return PagedTile{-1, 0};
 }
 
 // The key steps some row of a tile sees: the prefix's, then from the window of its first row to its last position.
@@ -119,12 +148,6 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
 template <typename T> __device__ __forceinline__ float only_not_finite(T bits) {
     const float v = Elem<T>::load(&bits);
     return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? v : 0.f;
-}
-
-// tanh for scores that end in bf16: an absolute error of about 2^-23
-__device__ __forceinline__ float paged_tanh_fast(float x) {
-    const float e = __builtin_amdgcn_exp2f(x * 2.885390081777927f);   // exp(2 x)
-    return 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
 }
 
 }  // namespace wisv
