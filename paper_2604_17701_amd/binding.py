@@ -377,32 +377,33 @@ class Context:
     def _stream_now(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self.device.index) or _NULL_STREAM
 
-    def _ints(self, name: str, t: torch.Tensor, shape) -> int:
-        if t.dtype is not torch.int32 or t.device != self.device or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on {self.device}")
+    def _ints(self, name: str, t: torch.Tensor, *shape) -> int:
+        if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != self.device.index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {self.device}")
         return t.data_ptr()
 
-    def _floats(self, name: str, t: torch.Tensor, shape) -> int:
-        if t.dtype is not torch.float32 or t.device != self.device or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on {self.device}")
+    def _floats(self, name: str, t: torch.Tensor, *shape) -> int:
+        if t.shape != shape or t.dtype is not torch.float32 or t.get_device() != self.device.index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape} on {self.device}")
         return t.data_ptr()
 
     def _rows(self, name: str, t: torch.Tensor, dtype, rows: int, head_dim: int):
         """(pointer, heads, row stride) of packed rows [rows, heads, head_dim]; rows may lie apart, heads may not."""
-        if t.dim() != 3 or t.dtype is not dtype or t.device != self.device or t.shape[0] != rows or t.shape[2] != head_dim:
+        shape = t.shape
+        if len(shape) != 3 or shape[0] != rows or shape[2] != head_dim or t.dtype is not dtype or t.get_device() != self.device.index:
             raise ValueError(f"{name} must be [{rows}, heads, {head_dim}] of {dtype} on {self.device}")
-        heads, (s0, s1, s2) = t.shape[1], t.stride()
-        if (s2 != 1 or (heads > 1 and s1 != head_dim)) and t.numel():
+        heads, (s0, s1, s2) = shape[1], t.stride()
+        if (s2 != 1 or (s1 != head_dim and heads > 1)) and t.numel():
             raise ValueError(f"the heads of a row of {name} must lie close together")
         return t.data_ptr(), heads, s0 if rows > 1 else heads * head_dim
 
     def _pools(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         """(pages, KV heads, page size, head_dim, wisv_dtype, page stride) of a pair of pools."""
-        dt, dev = k_pages.dtype, self.device
-        if (dt is not torch.bfloat16 and dt is not torch.float32) or v_pages.dtype is not dt or k_pages.device != dev \
-                or v_pages.device != dev or k_pages.dim() != 4:
-            raise ValueError(f"the pools must be bfloat16 or float32 tensors on {dev}, of one type")
-        n, g, ps, hd = k_pages.shape
+        dt, dev, shape = k_pages.dtype, self.device.index, k_pages.shape
+        if (dt is not torch.bfloat16 and dt is not torch.float32) or v_pages.dtype is not dt or k_pages.get_device() != dev \
+                or v_pages.get_device() != dev or len(shape) != 4:
+            raise ValueError(f"the pools must be bfloat16 or float32 tensors on {self.device}, of one type")
+        n, g, ps, hd = shape
         if ps & 7 or v_pages.shape != (n, g, ps >> 3, hd, 8):
             raise ValueError("the pools must be [pages, kv heads, page size, head_dim] and [pages, kv heads, page size / 8, head_dim, 8]")
         stride = g * ps * hd
@@ -434,10 +435,10 @@ class Context:
             used = slots + 4 * max_tokens
             ptrs = (p, kv, pos, slots, used, used + 4)
         else:
-            ptrs = [self._ints(n, t, (m,)) for n, t, m in zip(PagePlan._fields, out, sizes)]
-        args = wisv_paged_plan_args(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, (b,)),
-                                    self._ints("new_len", new_len, (b,)), self._ints("free_pages", free_pages, (n_free,)) or None,
-                                    self._ints("block_table", block_table, (b, width)), *ptrs, self._stream_now())
+            ptrs = [self._ints(n, t, m) for n, t, m in zip(PagePlan._fields, out, sizes)]
+        args = wisv_paged_plan_args(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, b),
+                                    self._ints("new_len", new_len, b), self._ints("free_pages", free_pages, n_free) or None,
+                                    self._ints("block_table", block_table, b, width), *ptrs, self._stream_now())
         rc = self._lib.wisv_paged_plan(self._h, C.byref(args))
         if rc:
             self._check(rc)
@@ -469,14 +470,14 @@ class Context:
         elif q_out is not None:
             raise ValueError("q_out without q")
         if positions is not None:
-            pp = self._ints("positions", positions, (rows,))
+            pp = self._ints("positions", positions, rows)
         if cos is not None or sin is not None:
             if cos is None or sin is None or pp is None or cos.dim() != 2:
                 raise ValueError("cos and sin come together, [n_rope, head_dim / 2], and need positions")
             n_rope = cos.shape[0]
-            cp, sp = self._floats("cos", cos, (n_rope, hd >> 1)), self._floats("sin", sin, (n_rope, hd >> 1))
+            cp, sp = self._floats("cos", cos, n_rope, hd >> 1), self._floats("sin", sin, n_rope, hd >> 1)
         args = wisv_paged_append_args(rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos, pp,
-                                      self._ints("slots", slots, (rows,)), cp, sp, k_pages.data_ptr(), v_pages.data_ptr(), stride,
+                                      self._ints("slots", slots, rows), cp, sp, k_pages.data_ptr(), v_pages.data_ptr(), stride,
                                       self._stream_now())
         rc = self._lib.wisv_paged_append(self._h, C.byref(args))
         if rc:
@@ -508,10 +509,10 @@ class Context:
         b, width = kv_len.numel(), block_table.shape[1]
         args = wisv_paged_attention_args(
             b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,
-            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, (b, width)),
-            self._ints("q_start", q_start, (b + 1,)), self._ints("kv_len", kv_len, (b,)),
-            None if prefix_len is None else self._ints("prefix_len", prefix_len, (b,)),
-            None if slopes is None else self._floats("slopes", slopes, (heads,)), None, 0, self._stream_now())
+            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, b, width),
+            self._ints("q_start", q_start, b + 1), self._ints("kv_len", kv_len, b),
+            None if prefix_len is None else self._ints("prefix_len", prefix_len, b),
+            None if slopes is None else self._floats("slopes", slopes, heads), None, 0, self._stream_now())
         ref = C.byref(args)
         if workspace is None:
             need = C.c_size_t()

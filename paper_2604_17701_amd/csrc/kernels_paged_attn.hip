@@ -449,7 +449,7 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     } else {
         // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 2.5 (its start and its
         // end), the join and its launch 5 and the parts' way through memory
-        const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / 32, a.batch) : a.batch) * a.G;
+        const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / (head_dim == 256 ? 16 : 32), a.batch) : a.batch) * a.G;
         const double unit = 128.0 * head_dim * (bf16 ? 2 : 4) / 36e3, part = (double)a.n_tokens * a.H * head_dim * 8 / 4e6;
         double best = 0;
         c.n_splits = 1;
@@ -469,7 +469,7 @@ template <typename T, int HD, int NQ> static void launch_rows(const PagedAttn &a
     else hipLaunchKernelGGL((k_paged_rows<T, HD, NQ, false>), grid, dim3(64 * rows_waves(HD, NQ)), 0, stream, a);
 }
 template <typename T, int HD> static void launch_rows_t(const PagedAttn &a, bool two, hipStream_t stream) {
-    if constexpr (sizeof(T) == 2 && HD == 128) return launch_rows<T, HD, 1>(a, stream);   // (row_limit)
+    if constexpr (HD == 256 || (sizeof(T) == 2 && HD == 128)) return launch_rows<T, HD, 1>(a, stream);   // (bf16, head_dim 128: row_limit)
     else return two ? launch_rows<T, HD, 2>(a, stream) : launch_rows<T, HD, 1>(a, stream);
 }
 template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim, bool two, hipStream_t stream) {
@@ -504,9 +504,13 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
     } else {
         a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
         const int64_t rows = (int64_t)a.rep * max_new;
-        a.tiles = rows > row_limit(bf16, head_dim);
-        if (bf16) launch_rows_d<bf16_t>(a, head_dim, rows > 16, stream);
-        else launch_rows_d<float>(a, head_dim, rows > 16, stream);
+        // Two query tiles per wave read the keys half as often; one where that leaves few workgroups (float, 5 requests of up to 37
+        // rows, 4 KV heads: 15.8 us and 12.8) and at head_dim 256, where two do not fit the registers (float, 23 prompts of 400, one
+        // KV head: 785 us and 634)
+        const bool two = rows > 16 && head_dim < 256 && ((int64_t)a.n_tokens * a.rep / 32 + 1) * a.G >= 32;
+        a.tiles = rows > (two ? row_limit(bf16, head_dim) : 16);
+        if (bf16) launch_rows_d<bf16_t>(a, head_dim, two, stream);
+        else launch_rows_d<float>(a, head_dim, two, stream);
     }
     if (a.n_splits > 1) {
         if (bf16) launch_join<bf16_t>(a, head_dim, stream);
