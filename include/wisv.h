@@ -295,7 +295,7 @@ int wisv_paged_plan(wisv_ctx *ctx, const wisv_paged_plan_args *args);
 /* Rotates the queries and keys of n_tokens rows and stores keys and values into their slots: with half = head_dim / 2,
  * c = cos[position][i], s = sin[position][i], the pair (x_i, x_{i + half}) becomes (x_i c - x_{i + half} s,
  * x_{i + half} c + x_i s), in float, rounded once.  Rows whose slot lies outside the pool store no key and no value (their
- * queries are rotated all the same); two rows with one slot leave either.  Positions outside the tables take the nearest
+ * queries are rotated all the same); of two rows with one slot either may leave an element there.  Positions outside the tables take the nearest
  * row of them.  q_out may be q (with the same stride). */
 typedef struct {
     int32_t n_tokens;            /* 0: nothing to do */
@@ -318,11 +318,12 @@ int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
  * rows of request b has position p = kv_len[b] - n + i and sees key j if j < kv_len[b] and
  *     j < prefix_len[b],  or  j <= p and (window == 0 or j > p - window).
  * Its score is x = scale * q.k, then softcap * tanh(x / softcap) if softcap > 0, then x + slopes[head] * (j - p) if slopes
- * are given; the output is the softmax-weighted sum of the values, and 0 for a row that sees no key.  Query head h reads KV
+ * are given; the output is the softmax-weighted sum of the values, and 0 for a row that sees no key (or none with a score
+ * above minus infinity).  Query head h reads KV
  * head h / (n_heads / n_kv_heads).
  * Keys and values that a row does not see do not reach its output, whatever they hold; a value that it sees and that is
  * not finite makes that feature of its output infinite or NaN.  Rows of q behind q_start[batch] are
- * neither read nor written.  kv_len beyond max_pages * page_size leaves the positions behind the table unseen.
+ * neither read nor written, nor are those before q_start[0].  kv_len beyond max_pages * page_size leaves the positions behind the table unseen.
  * max_new and max_len say how many new rows and how long a request is at most (0: unknown).  They choose how the work is
  * cut; requests beyond them are served all the same, more slowly.
  * Arithmetic: scores, softmax and sums in float; WISV_BF16 rounds once at the end, and probabilities enter the matrix cores as
@@ -333,11 +334,12 @@ int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
 typedef struct {
     int32_t batch;    /* 0: nothing to do */
     int32_t n_tokens; /* rows of q and out */
-    int32_t n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages, max_pages;
+    int32_t n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages;
+    int32_t max_pages; /* max_pages * page_size at most 2^30 */
     int32_t max_new, max_len;
     int32_t window;   /* 0: none */
     float scale;      /* 0: 1 / sqrt(head_dim) */
-    float softcap;    /* 0: none */
+    float softcap;    /* 0: none; else from 1e-30 to 16384 */
     const void *q;
     void *out;
     int64_t q_stride, out_stride; /* elements from row to row */

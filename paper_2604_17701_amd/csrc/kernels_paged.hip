@@ -101,7 +101,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_paged_plan(PagedPlan a) {
             if (f >= 0) {
                 const int have = (int)(((int64_t)c + ps - 1) >> a.page_shift), p = pos >> a.page_shift;
                 const int page = p < have ? a.block_table[(size_t)lo * a.max_pages + p] : a.free_pages[f + p - have];
-                if (page >= 0) slot = (page << a.page_shift) + (pos & (ps - 1));
+                if (page >= 0 && page <= INT32_MAX >> a.page_shift) slot = (page << a.page_shift) + (pos & (ps - 1));
             }
         }
         a.positions[t] = pos;
@@ -240,10 +240,17 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedAppend a, 
     }
 }
 
+static int64_t append_rot_wgs(const PagedAppend &a, bool bf16, int head_dim) {
+    const int64_t items = (int64_t)a.n_tokens * ((a.H + a.G + ROT_HEADS - 1) / ROT_HEADS) * (head_dim / 2 / (bf16 ? 8 : 4));
+    return (items + APPEND_THREADS - 1) / APPEND_THREADS;
+}
+static int64_t append_v_wgs(const PagedAppend &a) { return ((int64_t)a.n_tokens + V_TILE - 1) / V_TILE * a.G; }
+int64_t paged_append_threads(const PagedAppend &a, bool bf16, int head_dim) {
+    return (append_rot_wgs(a, bf16, head_dim) + append_v_wgs(a)) * APPEND_THREADS;
+}
 template <typename T, int HD> static void launch_append_t(const PagedAppend &a, hipStream_t stream) {
     const int rot_groups = (a.H + a.G + ROT_HEADS - 1) / ROT_HEADS;
-    const int64_t items = (int64_t)a.n_tokens * rot_groups * (HD / 2 / Pack<T>::N);
-    const int rot_wgs = (int)((items + APPEND_THREADS - 1) / APPEND_THREADS), v_wgs = (a.n_tokens + V_TILE - 1) / V_TILE * a.G;
+    const int rot_wgs = (int)append_rot_wgs(a, sizeof(T) == 2, HD), v_wgs = (int)append_v_wgs(a);
     hipLaunchKernelGGL((k_paged_append<T, HD>), dim3(rot_wgs + v_wgs), dim3(APPEND_THREADS), 0, stream, a, rot_groups, rot_wgs);
 }
 template <typename T> static void launch_append_d(const PagedAppend &a, int head_dim, hipStream_t stream) {

@@ -364,7 +364,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
     const int tid = threadIdx.x, group = tid / (TPI * ITEMS), in = tid % (TPI * ITEMS), d = in % TPI * 4;
     const int64_t item = (int64_t)blockIdx.x * ITEMS + in / TPI, row = item / a.H;
     const int h = item % a.H;
-    const bool live = row < min(a.q_start[a.batch], a.n_tokens);   // rows behind the last request stay as they are
+    const bool live = row >= a.q_start[0] && row < min(a.q_start[a.batch], a.n_tokens);   // other rows stay as they are
     if (GROUPS == 1 && !live) return;
     const int64_t at = (live ? row : 0) * a.H + h, step = (int64_t)a.n_tokens * a.H;
     float mx = -INFINITY, den = 0.f;
@@ -447,14 +447,14 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     } else {
-        // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 2.5 (its start and its
+        // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 6 (its start and its
         // end), the join and its launch 5 and the parts' way through memory
         const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / (head_dim == 256 ? 16 : 32), a.batch) : a.batch) * a.G;
         const double unit = 128.0 * head_dim * (bf16 ? 2 : 4) / 36e3, part = (double)a.n_tokens * a.H * head_dim * 8 / 4e6;
         double best = 0;
         c.n_splits = 1;
         for (int s = 1; s <= PAGED_MAX_SPLITS && (s == 1 || steps / s >= 2); ++s) {
-            const double cost = (double)((wgs * s + 255) / 256) * (unit * steps / s + 2.5) + (s > 1 ? 5 + s * part : 0);
+            const double cost = (double)((wgs * s + 255) / 256) * (unit * steps / s + 6) + (s > 1 ? 5 + s * part : 0);
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     }
@@ -483,7 +483,7 @@ template <typename T> static void launch_rows_d(const PagedAttn &a, int head_dim
 template <typename T, int HD> static void launch_join_t(const PagedAttn &a, hipStream_t stream) {
     constexpr int ALL = 1024 / HD;   // groups that a workgroup has for one (row, head)
     const int64_t items = (int64_t)a.n_tokens * a.H;
-    if (a.n_splits > 8) hipLaunchKernelGGL((k_paged_join<T, HD, ALL>), dim3((unsigned)items), dim3(256), 0, stream, a);
+    if (a.n_splits > 8 && items <= 1 << 16) hipLaunchKernelGGL((k_paged_join<T, HD, ALL>), dim3((unsigned)items), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((k_paged_join<T, HD, 1>), dim3((unsigned)((items + ALL - 1) / ALL)), dim3(256), 0, stream, a);
 }
 template <typename T> static void launch_join(const PagedAttn &a, int head_dim, hipStream_t stream) {

@@ -21,6 +21,7 @@ struct PagedAppend {
     const int32_t *positions, *slots;
     const float *cs, *sn;
 };
+int64_t paged_append_threads(const PagedAppend &a, bool bf16, int head_dim);   // of the launch, at most 2^32 - 1
 void launch_paged_append(const PagedAppend &a, bool bf16, int head_dim, hipStream_t stream);
 
 struct PagedAttn {

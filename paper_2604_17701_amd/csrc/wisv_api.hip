@@ -1143,13 +1143,12 @@ extern "C" int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *ar
                                     "their heads and are multiples of 16 bytes");
     if (p.q_out == p.q && p.n_heads && p.q_stride != p.q_out_stride)
         return fail(c, WISV_EINVAL, "wisv_paged_append: q_out is q with another stride");
-    // the grid: a thread per 16-byte piece of four heads
-    if ((int64_t)p.n_tokens * (p.n_heads + p.n_kv_heads + 3) * p.head_dim > (int64_t)1 << 38)
-        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_append: more elements than one launch covers (2^38)");
-    const OnDevice dev(c->cfg.device_id);
-    HIP_TRY(c, dev.err);
     const PagedAppend a{p.n_tokens, p.n_heads, p.n_kv_heads, p.n_rope, p.n_pages, log2_of(p.page_size), p.q, p.k, p.v, p.q_out, p.k_pages,
                         p.v_pages, p.q_stride, p.k_stride, p.v_stride, p.q_out_stride, page_stride, p.positions, p.slots, p.cos, p.sin};
+    if (paged_append_threads(a, p.dtype == WISV_BF16, p.head_dim) > UINT32_MAX)
+        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_append: more elements than one launch covers");
+    const OnDevice dev(c->cfg.device_id);
+    HIP_TRY(c, dev.err);
     launch_paged_append(a, p.dtype == WISV_BF16, p.head_dim, paged_stream(c, p.hip_stream));
     HIP_TRY(c, hipGetLastError());
     return WISV_OK;
@@ -1166,11 +1165,12 @@ static int paged_attention_args(Ctx *c, const wisv_paged_attention_args *args, P
         return fail(c, WISV_EINVAL, "wisv_paged_attention: %s", why);
     if (p.n_heads < 1 || p.n_heads > 1 << 16 || p.n_heads % p.n_kv_heads)
         return fail(c, WISV_EINVAL, "wisv_paged_attention: n_heads must be a multiple of n_kv_heads (and at most 65536)");
-    if (p.max_pages < 1 || (int64_t)p.max_pages * p.page_size > INT32_MAX)
-        return fail(c, WISV_EINVAL, "wisv_paged_attention: max_pages must be positive and max_pages * page_size at most 2^31 - 1");
+    if (p.max_pages < 1 || (int64_t)p.max_pages * p.page_size > 1 << 30)
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: max_pages must be positive and max_pages * page_size at most 2^30");
     if (p.max_new < 0 || p.max_len < 0 || p.window < 0) return fail(c, WISV_EINVAL, "wisv_paged_attention: max_new, max_len or window is negative");
-    if (!(p.softcap >= 0.f) || !isfinite(p.softcap) || !isfinite(p.scale))
-        return fail(c, WISV_EINVAL, "wisv_paged_attention: softcap must be finite and not negative, scale finite");
+    // (bf16 calls have a cap's tanh to 2^-23 of the cap: up to 2^14 that is within a probability's own rounding)
+    if ((p.softcap != 0.f && !(p.softcap >= 1e-30f && p.softcap <= 16384.f)) || !isfinite(p.scale))
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: softcap must be 0 or from 1e-30 to 16384, scale finite");
     const int64_t width = (int64_t)p.n_heads * p.head_dim;
     if (p.batch && p.n_tokens) {
         if (!rows_ok(p.q, p.q_stride, width, p.dtype) || !rows_ok(p.out, p.out_stride, width, p.dtype))
@@ -1178,11 +1178,14 @@ static int paged_attention_args(Ctx *c, const wisv_paged_attention_args *args, P
                                         "heads and are multiples of 16 bytes");
         if (!p.block_table || !p.q_start || !p.kv_len) return fail(c, WISV_EINVAL, "wisv_paged_attention: block_table, q_start or kv_len is NULL");
     }
-    if ((int64_t)p.n_tokens * p.n_heads > INT32_MAX / 4 || (int64_t)p.batch * p.n_kv_heads > INT32_MAX / 4)
-        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_attention: more rows than one launch covers (2^29 of rows x heads, or of requests x KV heads)");
+    // (512 threads for sixteen rows x heads and for every request's KV head, 2^32 in all)
+    if ((int64_t)p.n_tokens * p.n_heads > 1 << 26 || (int64_t)p.batch * p.n_kv_heads >= 1 << 21)
+        return fail(c, WISV_EUNSUPPORTED, "wisv_paged_attention: more than one launch covers (n_tokens * n_heads beyond 2^26 or batch * n_kv_heads "
+                                          "from 2^21)");
     *a = PagedAttn{};
     a->batch = p.batch; a->n_tokens = p.n_tokens; a->H = p.n_heads; a->G = p.n_kv_heads; a->rep = p.n_heads / p.n_kv_heads;
-    a->n_pages = p.n_pages; a->max_pages = p.max_pages; a->page_shift = log2_of(p.page_size); a->window = p.window;
+    a->n_pages = p.n_pages; a->max_pages = p.max_pages; a->page_shift = log2_of(p.page_size);
+    a->window = std::min(p.window, 1 << 30);   // (no position is further away; differences stay within an int)
     a->scale = p.scale != 0.f ? p.scale : 1.0f / sqrtf((float)p.head_dim);
     a->softcap = p.softcap;
     a->q = p.q; a->k_pages = p.k_pages; a->v_pages = p.v_pages; a->out = p.out;

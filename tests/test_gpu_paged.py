@@ -488,3 +488,143 @@ def test_steps_on_another_stream_and_two_workspaces(ctx):
     for i in range(2):
         for o in got[i]:
             assert torch.equal(o, alone[i])
+
+
+# ------------------------------------------------------------------------------------------------ more shapes and edges
+
+@pytest.mark.parametrize("dtype,dim,h,g", [(BF16, 128, 4, 1), (BF16, 64, 1, 1), (BF16, 256, 2, 1), (BF16, 32, 8, 2), (F32, 64, 2, 1)])
+@pytest.mark.parametrize("new", [16, 17, 31, 32, 33, 64, 127, 128, 129])
+def test_attention_around_the_tiles(ctx, dtype, dim, h, g, new):
+    """Rows that end before, at and behind tiles of 16, 32 and 128 rows; keys that end around a block of 64."""
+    for lens, news in (([new], [new]), ([new + 63], [new]), ([new + 64, 65, new + 1], [new, 2, new])):
+        q, kp, vp, table, starts = setup(dtype, dim, h, g, 16, lens, news, seed=new)
+        check_attention(ctx, q, kp, vp, table, starts, lens)
+
+
+@pytest.mark.parametrize("dtype,dim,h,g,news", [(BF16, 64, 40, 1, [1, 3]), (BF16, 128, 128, 1, [1, 2]), (BF16, 32, 96, 2, [2, 0]), (BF16, 256, 33, 1, [1, 2]),
+                                                (F32, 32, 130, 1, [1, 2])])
+def test_attention_with_more_query_heads_than_a_tile_has_rows(ctx, dtype, dim, h, g, news):
+    lens = [150, 40]
+    q, kp, vp, table, starts = setup(dtype, dim, h, g, 32, lens, news)
+    check_attention(ctx, q, kp, vp, table, starts, lens, softcap=8.0)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256, 512, 1024, 2048, 4096])
+@pytest.mark.parametrize("dtype,new", [(BF16, 1), (BF16, 50), (F32, 20)])
+def test_every_page_size(ctx, page, dtype, new):
+    h, g, dim, n = 4, 2, 64, 5000 if page > 256 else 700
+    lens = [n, new]
+    q, kp, vp, table, starts = setup(dtype, dim, h, g, page, lens, [new, new])
+    check_attention(ctx, q, kp, vp, table, starts, lens, window=600)
+    pos = np.arange(lens[0] - 40, lens[0])
+    slots = table[0][pos // page].astype(np.int64) * page + pos % page
+    check_append(ctx, dtype, dim, h, g, page, slots, kp.shape[0], pos % 50)
+
+
+@pytest.mark.parametrize("dtype,hi", [(BF16, 70), (F32, 40)])
+def test_attention_of_many_requests(ctx, dtype, hi):
+    """More requests than the search for a tile's owner takes at a time, idle ones among them."""
+    rng = np.random.default_rng(4)
+    batch = 1100
+    news = np.where(rng.random(batch) < 0.4, 0, rng.integers(1, 4, batch))
+    news[[3, 511, 512, 513, 1023, 1024, 1099]] = hi
+    lens = news + rng.integers(0, 60, batch)
+    q, kp, vp, table, starts = setup(dtype, 32, 2, 1, 16, lens, news)
+    check_attention(ctx, q, kp, vp, table, starts, list(lens))
+
+
+@pytest.mark.parametrize("dtype,lens,news", [(BF16, [2000, 90], [1, 2]), (BF16, [900, 90], [80, 50]), (F32, [1500, 70], [3, 40])])
+def test_attention_leaves_the_rows_before_the_first_request(ctx, dtype, lens, news):
+    q, kp, vp, table, starts = setup(dtype, 64, 4, 1, 32, lens, news)
+    pad = 7
+    padded = torch.cat([torch.full_like(q[:1], float("nan")).expand(pad, -1, -1), q]).contiguous()
+    out = torch.full_like(padded, 5.0)
+    alone = ctx.wisv_paged_attention(q, kp, vp, ints(table), ints(starts), ints(lens), max(news), max(lens))
+    got = ctx.wisv_paged_attention(padded, kp, vp, ints(table), ints(starts + pad), ints(lens), max(news), max(lens), out=out)
+    assert (got[:pad] == 5.0).all()
+    # (tiles do not move with the rows: the same products in the same order, but perhaps another cut of the keys)
+    ref_out, mass, top = ref.attention(f64(q), f64(kp), f64(vp), table, starts, lens)
+    lim = limits(dtype, 64, max(lens), ref_out, mass, top, 0.0)
+    assert (np.abs(f64(got[pad:]) - ref_out) <= lim).all() and (np.abs(f64(alone) - ref_out) <= lim).all()
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, 3), (BF16, 60), (F32, 40)])
+def test_attention_keys_that_are_no_numbers_reach_only_the_rows_that_see_them(ctx, dtype, new):
+    lens, page = [100], 32
+    q, kp, vp, table, starts = setup(dtype, 128, 4, 2, page, lens, [new])
+    out, mass, top = ref.attention(f64(q), f64(kp), f64(vp), table, starts, lens)
+    at = 100 - new + new // 2
+    kp[int(table[0, at // page]), 1, at % page, 5] = float("nan")
+    got = f64(ctx.wisv_paged_attention(q, kp, vp, ints(table), ints(starts), ints(lens), new, 100))
+    lim = limits(dtype, 128, 100, out, mass, top, 0.0)
+    p = 100 - new + np.arange(new)
+    assert np.isnan(got[p >= at][:, 2:]).all()                                     # the KV head's own query heads
+    assert (np.abs(got - out)[:, :2] <= lim[:, :2]).all() and (np.abs(got - out)[p < at] <= lim[p < at]).all()
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, 2), (BF16, 40), (F32, 33)])
+@pytest.mark.parametrize("kw", [dict(window=2 ** 31 - 1), dict(softcap=1e-3), dict(softcap=1e4), dict(scale=30.0), dict(scale=1e-6),
+                                dict(window=5, prefix=[2 ** 31 - 1, -4]), dict(window=70, prefix=[130, 33], slopes=[0.5, 0.0, -0.25, 3.0])],
+                         ids=lambda k: "-".join(map(str, k)))
+def test_attention_extreme_settings(ctx, dtype, new, kw):
+    lens, news = [400, 90], [new, min(new, 9)]
+    q, kp, vp, table, starts = setup(dtype, 64, 4, 2, 16, lens, news)
+    check_attention(ctx, q, kp, vp, table, starts, lens, **kw)
+
+
+@pytest.mark.parametrize("dim,softcap,slopes,new", [(32, 9.0, True, 40), (256, 3.0, True, 50), (64, 0.0, True, 1), (128, 7.0, False, 6)])
+def test_attention_captured_before_it_has_run(ctx, dim, softcap, slopes, new):
+    """A graph captured as the first call of its kind, replayed with other lengths and queries, eager work between the replays."""
+    h, g, page, batch = 4, 2, 16, 2
+    q, kp, vp, table, starts = setup(BF16, dim, h, g, page, [300, 300], [new, new])
+    t, qs, kl = ints(table), ints(starts), ints([300, 300])
+    sl = torch.linspace(0.1, 0.4, h, device=DEV) if slopes else None
+    out = torch.zeros_like(q)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ctx.wisv_paged_attention(q, kp, vp, t, qs, kl, new, 300, softcap=softcap, slopes=sl, out=out)
+    for i, lens in enumerate(([300, 300], [17 + new, 250], [new, 299])):
+        kl.copy_(ints(lens))
+        q.copy_(normal(50 + i, tuple(q.shape), BF16, 2.0))
+        out.zero_()
+        graph.replay()
+        _ = torch.randn(64, device=DEV).sum().item()
+        eager = ctx.wisv_paged_attention(q, kp, vp, t, qs, kl, new, 300, softcap=softcap, slopes=sl)
+        assert torch.equal(out, eager)
+        check_attention(ctx, q, kp, vp, table, starts, lens, softcap=softcap, slopes=None if sl is None else f64(sl), max_new=new, max_len=300)
+
+
+def test_two_graphs_replayed_at_once(ctx):
+    """Graphs captured apart have workspaces apart: replayed on two streams at once they give what they give alone."""
+    jobs, graphs, outs = [], [], []
+    for seed, lens, news in ((1, [4000, 300], [3, 1]), (2, [3500, 40], [2, 2])):
+        q, kp, vp, table, starts = setup(BF16, 128, 8, 2, 32, lens, news, seed=seed)
+        args = (q, kp, vp, ints(table), ints(starts), ints(lens), max(news), max(lens))
+        alone = ctx.wisv_paged_attention(*args)
+        out, graph = torch.zeros_like(alone), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            ctx.wisv_paged_attention(*args, out=out)
+        jobs.append((args, alone))
+        graphs.append(graph)
+        outs.append(out)
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, gr in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                gr.replay()
+        torch.cuda.synchronize()
+        for o, (_, alone) in zip(outs, jobs):
+            assert torch.equal(o, alone)
+
+
+def test_plan_with_entries_that_no_pool_has(ctx):
+    """Table entries and free pages so large that their slots would not fit an int are left without a slot."""
+    t = [[2 ** 31 - 1, -1], [2 ** 27, -1], [2 ** 27 - 1, -1]]
+    dev = ints(t)
+    plan = ctx.wisv_paged_plan(ints([3, 3, 3]), ints([2, 2, 2]), ints([]).reshape(-1), dev, 16, 6)
+    assert plan.slots.tolist() == [-1, -1, -1, -1, (2 ** 27 - 1) * 16 + 3, (2 ** 27 - 1) * 16 + 4] and plan.status.tolist() == [0, 0, 0]

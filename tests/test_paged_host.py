@@ -173,3 +173,16 @@ def test_oracle_attention_by_hand():
     assert np.allclose(call(slopes=[np.log(3.0)]), [0.4, 3.6])                    # the nearer key gains another factor of 3
     out = ref.attention(np.ones((3, 1, 2)), kp, vp, [[0]], [0, 3], [2], scale=1.0)[0]
     assert (out[0] == 0).all() and np.allclose(out[1, 0], [4.0, 0.0])             # the first row lies before the cache
+
+
+def test_calls_that_one_launch_does_not_cover_are_refused(stub):
+    run(stub, '''
+        assert attn(n_tokens=1 << 25, n_heads=4) == B.WISV_EUNSUPPORTED and "2^26" in text()
+        assert attn(batch=1 << 20, n_kv_heads=2) == B.WISV_EUNSUPPORTED and "2^21" in text()
+        assert attn(max_pages=1 << 27) == B.WISV_EINVAL and "2^30" in text()
+        for cap in (1e-37, 16385.0, float("inf"), float("nan"), -2.0):
+            assert attn(softcap=cap) == B.WISV_EINVAL and "softcap" in text(), cap
+        assert append(n_tokens=1 << 30) == B.WISV_EUNSUPPORTED and "one launch" in text()
+        assert log() == []
+        assert attn(n_tokens=1 << 24, n_heads=4, max_new=8, max_pages=2) == 0 and attn(window=2**31 - 1) == 0
+    ''')
