@@ -461,7 +461,7 @@ class Context:
         if q is not None:
             qp, heads, qs = self._rows("q", q, dt, rows, hd)
             if q_out is None:
-                q_out = torch.empty((rows, heads, hd), dtype=dt, device=self.device)
+                q_out = torch.empty_like(q)   # (contiguous: the heads of a row of q lie close together)
                 qop, qos = q_out.data_ptr(), heads * hd
             else:
                 qop, oh, qos = self._rows("q_out", q_out, dt, rows, hd)
@@ -498,7 +498,7 @@ class Context:
         rows, dt = q.shape[0], k_pages.dtype
         qp, heads, qs = self._rows("q", q, dt, rows, hd)
         if out is None:
-            out = torch.empty_like(q) if qs == heads * hd else torch.empty((rows, heads, hd), dtype=dt, device=self.device)
+            out = torch.empty_like(q)   # (contiguous: the heads of a row of q lie close together)
             op, os_ = out.data_ptr(), heads * hd
         else:
             op, oh, os_ = self._rows("out", out, dt, rows, hd)

@@ -19,6 +19,7 @@
 namespace wisv {
 
 typedef float paged_f16 __attribute__((ext_vector_type(16)));
+typedef __bf16 paged_bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int BLOCK = 64;   // positions
 
 __device__ __forceinline__ paged_f16 mfma32(paged_u4 a, paged_u4 b, paged_f16 c) {
@@ -185,11 +186,13 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
         if (see_none(key0)) continue;
         // ---- scores: register r of tile i is key 32 i + 16 (r / 8) + 8 h2 + r % 8
         paged_f16 x[2];
+        __builtin_amdgcn_s_setprio(1);   // products first: the other workgroup's wave has its exponentials meanwhile
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 x[i] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + ((kaddr + stage * BUF) ^ (32 * t)) + i * 32 * HD * 2), q[t], t ? x[i] : zero);
+        __builtin_amdgcn_s_setprio(0);
         if (MODS != PLAIN) {   // into units of ln 2, with cap and bias (PLAIN scales them with the exponentials)
             const float near = slope * (float)(key0 + 8 * h2 - pos);
 #pragma unroll
@@ -216,12 +219,16 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
                 }
         }
         // (the maximum that lets NaN through is one instruction for two values; a row with one is NaN whatever the reference)
-        float mx = x[0][0];
+        float part[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i) {
+            part[i] = x[i >> 1][8 * (i & 1)];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, x[i][r]);
-        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
+            for (int r = 1; r < 8; ++r) part[i] = __builtin_elementwise_maximum(part[i], x[i >> 1][8 * (i & 1) + r]);
+        }
+        float mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(part[0], part[1]), __builtin_elementwise_maximum(part[2], part[3]));
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);   // the lower and the upper lanes', in all
+        mx = __builtin_elementwise_maximum(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
         if (MODS == PLAIN) mx *= scale2;
         if (__any(mx > m_ref + 8.f)) {
             const float m_new = fmaxf(m_ref, mx);
@@ -239,12 +246,13 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             for (int w = 0; w < 4; ++w) {
                 const float x0 = x[kc >> 1][8 * (kc & 1) + 2 * w], x1 = x[kc >> 1][8 * (kc & 1) + 2 * w + 1];
                 const float e0 = __builtin_amdgcn_exp2f(MODS ? x0 - sub : fmaf(x0, scale2, -sub)), e1 = __builtin_amdgcn_exp2f(MODS ? x1 - sub : fmaf(x1, scale2, -sub));
-                l_run[0] += e0;
-                l_run[1] += e1;
-                p[kc][w] = f32x2_to_bf16x2(e0, e1);
+                const uint32_t both = f32x2_to_bf16x2(e0, e1);
+                p[kc][w] = both;
+                // (the sum of what the product weighs with: rounding errors that all probabilities share cancel)
+                l_run[w & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(paged_bf16x2, both), __builtin_bit_cast(paged_bf16x2, 0x3f803f80u), l_run[w & 1], false);
             }
         };
-        // a run of sixteen keys' products, and the next run's exponentials beside them; the other workgroup's wave yields
+        // a run of sixteen keys' products, and the next run's exponentials beside them
         probs(0);
         __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
