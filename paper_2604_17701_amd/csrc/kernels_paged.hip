@@ -9,7 +9,7 @@ namespace wisv {
 // ------------------------------------------------------------------------------------------ step planning
 // One launch: every workgroup scans the lengths for itself (two prefix sums over the requests, kept in LDS) and then
 // writes its share of the table and of the tokens; no workgroup waits for another.  Bound by the latency of launch,
-// loads and scan.
+// loads and scan: 5.5 us for 16 requests of 6 tokens, 6.2 for 512 with 22171 (a launch that does nothing takes 2.3).
 constexpr int PLAN_THREADS = 256;
 
 // exclusive prefix sum over the workgroup's threads
@@ -115,7 +115,8 @@ void launch_paged_plan(const PagedPlan &a, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------ rotate and append
-// Bound by HBM: every element is read once and written once.  Two kinds of workgroups in one launch:
+// Bound by HBM: every element is read once and written once (2483 rows of 32 / 8 heads of 128 in bf16, 62 MB: 12.6 us = 4.9 TB/s, the rate of a
+// large copy; four rows 3.3 us).  Two kinds of workgroups in one launch:
 //   q and k   a thread owns one 16-byte piece of a head's first half and its partner in the second half, for up to
 //             ROT_HEADS heads of a token whose rotary factors it reads once;
 //   v         a tile of 64 tokens x one KV head goes through LDS, since the pool keeps eight positions of a feature

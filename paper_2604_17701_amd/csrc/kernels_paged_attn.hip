@@ -1,9 +1,10 @@
-// Attention of a chunk of new tokens over the paged cache.
+// Attention of a chunk of new tokens over the paged cache: few rows per request (or float), the join of split keys, and the
+// choice between this kernel and kernels_paged_prompt.hip's.
 //
-// The rows of a request and KV head - its new tokens x the query heads that share the KV head, token by token - are cut
-// into tiles of 16 NQ rows, so that every cached byte meets a whole tile.  One workgroup = (split of the keys, KV head,
-// request); its waves take steps of 32 (bf16) or 16 (float) keys in turn and never meet before the end: keys and values
-// go from the pages straight into matrix operands.
+// k_paged_rows.  The rows of a request and KV head - its new tokens x the query heads that share the KV head, token by
+// token - are cut into tiles of 16 NQ rows, so that every cached byte meets a whole tile.  One workgroup = (split of the keys,
+// KV head, request or tile); its waves take steps of 32 (bf16) or 16 (float) keys in turn and never meet before the end: keys
+// and values go from the pages straight into matrix operands.
 //   S^T = K Q^T   A operand: keys.  The rows are dealt so that lane group g of 16 lanes ends up with the scores of E
 //                 consecutive keys (8, or 4) of each of 16 queries;
 //   O^T += V^T P^T  those E probabilities are, as they stand, the B operand, and the A operand is one 16-byte load per
@@ -11,6 +12,12 @@
 // The softmax keeps a running maximum and sum in float; waves are joined in LDS, splits of the keys by k_paged_join.
 // bf16: probabilities enter the matrix cores as two terms p = hi + lo, |p - hi - lo| <= 2^-17 p (what bounds this kernel
 // is memory, the second term is free).  float: 16x16x4 float products throughout.
+// Bound by bytes: 36 GB/s into one CU, about 6 TB/s into all; by latency below 100 KB per CU (a launch that reads next to nothing
+// takes 6.4 us), and float prompts by the float matrix rate.  Kernel traces: one token over 131072 positions, 32 / 8 heads of 128
+// (537 MB, 32 splits) 98 us = 5.5 TB/s; 36 tokens in windows of 4096, 16 / 8 heads of 256 (376 MB, ragged) 86 us = 4.4 TB/s; four
+// rows over 516 positions, 32 / 8 heads of 128 (2.2 MB, 4 splits) 8.7 us; a float prompt of 1024 behind 1024, 32 / 8 heads of 128,
+// 327 us = 79 TFLOP/s of 153.  Keys and values of one step in the same registers, so that two waves share a SIMD at head_dim
+// 256, spill (99 us -> 155).
 #include "paged.h"
 
 namespace wisv {
@@ -355,7 +362,8 @@ __global__ __launch_bounds__(64 * rows_waves(HD, NQ)) void k_paged_rows(PagedAtt
 
 // out = sum_s 2^(m_s - m*) o_s / sum_s 2^(m_s - m*) l_s over the splits that saw a key.  A thread owns four features of a (row,
 // head) and every GROUPS-th split, four of which are on their way at a time; the groups' sums are added in order.  GROUPS 1 fills
-// the chip when there are many rows, the whole workgroup on one (row, head) is for few rows of many splits.
+// the chip when there are many rows, the whole workgroup on one (row, head) is for few rows of many splits (one row of 32 heads,
+// 32 splits: 4.7 us; a wave per (row, head) that takes one split after the other 22.9).
 template <typename T, int HD, int GROUPS>
 __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
     constexpr int TPI = HD / 4, ITEMS = 256 / (TPI * GROUPS), AHEAD = 4;
@@ -437,18 +445,21 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     if (c.prompt) {
         // Workgroups run two to a CU (head_dim 256: one).  Splitting the keys fills a chip, or the last of its rounds, that is not
         // full.  In steps of 64 keys, about 2 us each: a split costs six (its start, its way to the join), the join three and
-        // the parts' way through memory
+        // the parts' way through memory.  us per call: six prompts of up to 777 behind 900, 28 / 4 heads of 64, 1 split 43, 2 (taken)
+        // 38, 3 35, 4 42; one of 723 behind 20990, 56 / 8 of 64, 538, 562, 415, 4 (taken) 450; two of 2048 behind 6144, 32 / 8 of 128,
+        // 1 (taken) 472, 2 535
         const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = head_dim == 256 ? 256 : 512;
         const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;
         double best = 0;
         c.n_splits = 1;
-        for (int s = 1; s <= 16 && (s == 1 || steps / s >= 4); ++s) {
+        for (int s = 1; s <= 32 && (s == 1 || steps / s >= 2); ++s) {
             const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + 0.25) * ((double)steps / s + 6) + (s > 1 ? 3 + s * part : 0);
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     } else {
         // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 6 (its start and its
-        // end), the join and its launch 5 and the parts' way through memory
+        // end), the join and its launch 5 and the parts' way through memory.  us per call: 36 tokens in windows of 4096, 16 / 8 heads
+        // of 256, 1 split 117, 2 96, 3 96, 4 (taken) 92, 6 102; 64 blocks of 8 rows over 8192, 32 / 8 of 128, 1 376, 2 392, 4 418
         const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / (head_dim == 256 ? 16 : 32), a.batch) : a.batch) * a.G;
         const double unit = 128.0 * head_dim * (bf16 ? 2 : 4) / 36e3, part = (double)a.n_tokens * a.H * head_dim * 8 / 4e6;
         double best = 0;

@@ -1,19 +1,28 @@
 // Attention of many rows over the paged cache (bf16): prompts, and blocks of more rows than k_paged_rows takes at once.
 //
-// Bound by the matrix cores.  A workgroup takes 32 NW rows of a request and KV head (its new tokens x the query heads that
-// share the KV head), 32 per wave; keys and values pass through LDS in blocks of 64 positions, two buffers deep, loaded
-// straight from the pages (global_load_lds, 16 bytes a lane; a wave fetches the keys and the values of the same few
-// positions, so that it needs one page number).  On 32x32x16 products:
+// A workgroup takes 128 rows of a request and KV head (its new tokens x the query heads that share the KV head), 32 per wave; keys
+// and values pass through LDS in blocks of 64 positions, a ring of them, loaded straight from the pages (global_load_lds, 16 bytes
+// a lane; a wave fetches the keys and the values of the same sixteen positions, which lie in one page).  On 32x32x16 products:
 //   S^T = K Q^T    the A operand's rows are dealt (bits 2 and 3 of the row swapped) so that a lane's sixteen scores of a tile are
 //                  two runs of eight consecutive keys of one query ...
 //   O^T += V^T P^T ... which are, rounded to bf16, the B operand as they stand; the A operand is one 16-byte LDS read from the V
 //                  pool's own order.
-// Keys lie in LDS with their 16-byte chunks exchanged by an XOR of the row, so that neither operand's reads meet in a bank.
-// A query's scores lie in two lanes: a maximum costs one exchange.  The running maximum is a reference that moves only when a
-// score exceeds it by 2^8 (sums and outputs are float: nothing is lost by a reference that is too low), so that rescaling the
-// outputs is rare.
-// Probabilities enter the product as one bf16 term, an error of 2^-8 relative each and of about 2^-9.3 in the mean, like that of the
-// output's own rounding; a second term would cost half as many matrix instructions again.
+// Keys lie in LDS with their 16-byte chunks exchanged by an XOR of the row, so that neither operand's reads meet in a bank
+// (SQ_LDS_BANK_CONFLICT 0).  A query's scores lie in two lanes: a maximum costs one exchange.  The running maximum is a reference that
+// moves only when a score exceeds it by 2^8 (sums and outputs are float: nothing is lost by a reference that is too low), so that
+// rescaling the outputs is rare.
+// Probabilities enter the product as one bf16 term, an error of at most 2^-8 relative each, in the mean like that of the output's own
+// rounding: the error against 64 bits is 1.1 to 1.35 times that of a result rounded once.  Two terms cost 478 -> 600 us (below).
+//
+// Bound by the matrix cores and the vector unit, which a SIMD's two waves, of different workgroups, overlap: the waves of one workgroup
+// run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 467 = 1.03 PFLOP/s, of
+// 64 (241 GFLOP) 292, 16 / 8 of 256 (481 GFLOP) 679; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 188: a cap is two
+// transcendentals a score more.  With up to 32 rows per request it is bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16
+// GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at head_dim 64, 1.4 at 128, 2.9 at 256, spread over loads, products,
+// exponentials and maxima.
+// Two workgroups of four waves against one of eight with the keys loaded half as often: 503 and 499 us for the prompts above, six of up
+// to 777 behind 900, 28 / 4 heads of 64, with a bias 53 and 72.  Priority to the phases of products: 481 -> 460, one of 723 behind 20990,
+// 56 / 8 of 64, with a cap 464 -> 436.  The next block's scores beside this block's exponentials in one wave, blocks of 32: 655 -> 735.
 #include "paged.h"
 
 namespace wisv {
@@ -31,7 +40,7 @@ __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, co
 }
 
 constexpr int PROMPT_WAVES = 4;
-// Blocks in LDS, 64 KB or (head_dim 256, whose registers allow one workgroup per CU) 128
+// Blocks in LDS, 64 KB or (head_dim 256, whose registers allow one workgroup per CU) 128; rings of twice as many were no faster
 constexpr int prompt_stages(int hd) { return hd == 256 ? 2 : 256 / hd; }
 constexpr size_t prompt_lds(int hd) { return (size_t)prompt_stages(hd) * 2 * BLOCK * hd * 2; }
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
@@ -39,7 +48,7 @@ enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 template <int HD, int MODS>
 __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_prompt(PagedAttn a) {
     extern __shared__ __align__(16) unsigned char lds[];   // [STAGES][K, V][BLOCK * HD]
-    constexpr int NWV = PROMPT_WAVES, ROWS = 32 * NWV, CPR = HD / 8, QT = HD / 16, OT = HD / 32, STAGES = prompt_stages(HD);
+    constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / 8, QT = HD / 16, OT = HD / 32, STAGES = prompt_stages(HD);
     constexpr float LOG2E = 1.4426950408889634f;
     constexpr int HALF = BLOCK * HD * 2, BUF = 2 * HALF;               // bytes
     constexpr int LOADS = HD / 32, WAITS = 2 * LOADS;                  // loads of 1 KB that sixteen positions take of either pool, and of both
@@ -78,7 +87,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
     bool hole = false;
     if (s_begin < s_end) {
         const int p0 = (real(s_begin) * BLOCK) >> a.page_shift, p1 = (min((real(s_end - 1) + 1) * BLOCK, rq.n_keys) - 1) >> a.page_shift;
-        for (int p = p0 + tid; p <= p1; p += 64 * NWV) hole |= (unsigned)a.block_table[(int64_t)b * a.max_pages + p] >= (unsigned)a.n_pages;
+        for (int p = p0 + tid; p <= p1; p += 64 * PROMPT_WAVES) hole |= (unsigned)a.block_table[(int64_t)b * a.max_pages + p] >= (unsigned)a.n_pages;
     }
     hole = __syncthreads_or(hole);
 
@@ -168,7 +177,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             // The same holds for values that only some rows see: those that are not finite are taken out and added at the end.
             const uint32_t ok = runs_there(key0);
             uint32_t out = 0;
-            for (int i = tid; i < BLOCK * HD / 8; i += 64 * NWV) {
+            for (int i = tid; i < BLOCK * HD / 8; i += 64 * PROMPT_WAVES) {
                 const int group = i / HD, n = ok >> (group >> 1) & 1 ? rq.n_keys - (key0 + 8 * group) : 0;   // of the group's eight keys
                 paged_u4 *to = reinterpret_cast<paged_u4 *>(lds + stage * BUF + HALF) + i;
                 paged_u4 v = *to;
@@ -317,9 +326,9 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
 int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
 template <int HD, int MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
-    static bool allowed[MAX_DEVICES];
+    static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
     const size_t lds = prompt_lds(HD);
-    if (lds > 60 * 1024 && !(device >= 0 && device < MAX_DEVICES && allowed[device])) {
+    if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
             (void)hipGetLastError();
             return "the device refuses the kernel's LDS request";

@@ -36,7 +36,7 @@ struct PagedAttn {
     const float *slopes;
     float *po, *pm, *pl;           // n_splits > 1: [split][n_tokens][H][head_dim], [split][n_tokens][H]; pm in units of ln 2
 };
-constexpr int PAGED_MAX_SPLITS = 64;   // the kernel that joins them gives each a lane
+constexpr int PAGED_MAX_SPLITS = 64;
 // What a call will launch, from the sizes and the hints alone
 struct PagedCut {
     bool prompt;                   // k_paged_prompt, or k_paged_rows

@@ -628,3 +628,25 @@ def test_plan_with_entries_that_no_pool_has(ctx):
     dev = ints(t)
     plan = ctx.wisv_paged_plan(ints([3, 3, 3]), ints([2, 2, 2]), ints([]).reshape(-1), dev, 16, 6)
     assert plan.slots.tolist() == [-1, -1, -1, -1, (2 ** 27 - 1) * 16 + 3, (2 ** 27 - 1) * 16 + 4] and plan.status.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("dtype,news", [(BF16, [1, 2, 1]), (BF16, [50, 3, 20]), (F32, [9, 1, 40])])
+def test_attention_over_pages_that_requests_share(ctx, dtype, news):
+    """Requests whose tables begin with the same pages (a common prompt), and a page that stands twice in one row."""
+    lens, page = [150, 90, 200], 16
+    q, kp, vp, table, starts = setup(dtype, 64, 4, 2, page, lens, news)
+    table[1, :4] = table[0, :4]
+    table[2, :3] = table[0, :3]
+    table[2, 7] = table[2, 5]
+    check_attention(ctx, q, kp, vp, table, starts, lens)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_append_of_two_rows_with_one_slot_leaves_either(ctx, dtype):
+    kp, vp = pools(4, 2, 16, 64, dtype)
+    k, v = normal(1, (70, 2, 64), dtype), normal(2, (70, 2, 64), dtype)
+    before = kp.clone(), vp.clone()
+    ctx.wisv_paged_append(None, k, v, None, ints([21] * 70), kp, vp)
+    assert (k == kp[1, :, 5]).any(0).all() and (v == vp[1, :, 0, :, 5]).any(0).all()
+    kp[1, :, 5], vp[1, :, 0, :, 5] = before[0][1, :, 5], before[1][1, :, 0, :, 5]
+    assert torch.equal(kp, before[0]) and torch.equal(vp, before[1])

@@ -186,3 +186,33 @@ def test_calls_that_one_launch_does_not_cover_are_refused(stub):
         assert log() == []
         assert attn(n_tokens=1 << 24, n_heads=4, max_new=8, max_pages=2) == 0 and attn(window=2**31 - 1) == 0
     ''')
+
+
+def test_a_device_that_refuses_the_lds_is_an_error(stub):
+    """A prompt's kernel wants 64 KB of LDS or more: a device that refuses says so before anything is enqueued, and the next
+    call is not blamed for it."""
+    run(stub, '''
+        many = dict(n_tokens=100, max_new=90)
+        stub.stub_refuse_lds(1)
+        assert attn(**many) == B.WISV_EHIP and "LDS" in text() and log() == []
+        assert attn() == 0 and len(log()) == 1            # few rows need no such kernel
+        stub.stub_refuse_lds(0)
+        stub.stub_log_clear()
+        assert attn(**many) == 0 and any("prompt" in l for l in log()), (text(), log())
+    ''')
+
+
+def test_which_kernel_serves_which_rows(stub):
+    run(stub, '''
+        def served(**kw):
+            stub.stub_log_clear()
+            need_ = need(**kw)
+            assert attn(**kw, workspace=P if need_ else None, workspace_bytes=need_) == 0, text()
+            return "".join("p" if "prompt" in l else "j" if "join" in l else "r" if "rows" in l else "?" for l in log())
+        assert served(max_new=5, n_tokens=10) == "r" and served(max_new=5, n_tokens=10, dtype=0) == "r"
+        assert served(max_new=17, n_tokens=20) == "p" and served(max_new=17, n_tokens=20, dtype=0) == "r"    # 34 rows per KV head
+        wide = dict(head_dim=128, q_stride=512, out_stride=512)
+        assert served(max_new=8, n_tokens=8, **wide) == "r" and served(max_new=9, n_tokens=9, **wide) == "p"
+        long = dict(batch=1, max_pages=4096, max_len=65536)
+        assert served(n_tokens=1, max_new=1, **long) == "rj" and served(n_tokens=40, max_new=40, **long) == "pj"
+    ''')
