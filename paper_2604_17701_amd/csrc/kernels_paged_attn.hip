@@ -438,7 +438,13 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     PagedCut c;
     const int64_t rows = (int64_t)a.rep * max_new;
     const bool many = rows > row_limit(bf16, head_dim);
-    c.prompt = bf16 && many;
+    // Float takes k_paged_prompt's 128 rows where they fill its tiles and the chip: with half the chip's CUs or more, and tiles that a
+    // request of average length fills to three quarters or more.  us per call, k_paged_rows and k_paged_prompt: two prompts of 1024
+    // behind 1024, 32 / 8 heads of 128, 605 and 518; one of 2048 behind 20000, 8 / 2 of 128, 1707 and 1357; 64 of 100 behind 100, 4 / 4
+    // of 64, 46 and 35; too few: one of 200 behind 900, 32 / 8 of 128, 57 and 58; 160 rows each: 24 of 40 tokens behind 4000, 32 / 8 of
+    // 64, 338 and 514; head_dim 32: 30 of 500 behind 500, 8 / 2, 157 and 167
+    const int64_t all_rows = (int64_t)a.n_tokens * a.rep, tiles_each = (all_rows + 128 * (int64_t)a.batch - 1) / (128 * (int64_t)a.batch);
+    c.prompt = many && (bf16 || (head_dim >= 64 && all_rows / 128 * a.G >= 128 && all_rows >= 96 * tiles_each * a.batch));
     // positions that a tile's rows see at most: a window's are those of its first row and what its rows span
     const int reach = a.window ? (int)std::min<int64_t>(max_len, (int64_t)a.window + 64 + (c.prompt ? 128 / a.rep : max_new)) : max_len;
     const int64_t steps = (reach + 63) / 64;
@@ -449,11 +455,12 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
         // 38, 3 35, 4 42; one of 723 behind 20990, 56 / 8 of 64, 538, 562, 415, 4 (taken) 450; two of 2048 behind 6144, 32 / 8 of 128,
         // 1 (taken) 472, 2 535
         const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = head_dim == 256 ? 256 : 512;
+        const double fixed = bf16 ? 1 : 18.0 / head_dim;
         const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;
         double best = 0;
         c.n_splits = 1;
         for (int s = 1; s <= 32 && (s == 1 || steps / s >= 2); ++s) {
-            const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + 0.25) * ((double)steps / s + 6) + (s > 1 ? 3 + s * part : 0);
+            const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + 0.25) * ((double)steps / s + 6 * fixed) + (s > 1 ? (3 + s * part) * fixed : 0);
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     } else {
@@ -510,8 +517,8 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
     const PagedCut cut = paged_cut(a, bf16, head_dim, max_new, max_len);
     a.n_splits = cut.n_splits;
     if (cut.prompt) {
-        a.split_steps = cut.split_steps;
-        if (const char *why = launch_paged_prompt(a, head_dim, device, stream)) return why;
+        a.split_steps = cut.split_steps * (bf16 ? 1 : 2);
+        if (const char *why = launch_paged_prompt(a, bf16, head_dim, device, stream)) return why;
     } else {
         a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
         const int64_t rows = (int64_t)a.rep * max_new;

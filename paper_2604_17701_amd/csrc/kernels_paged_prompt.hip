@@ -1,8 +1,9 @@
-// Attention of many rows over the paged cache (bf16): prompts, and blocks of more rows than k_paged_rows takes at once.
+// Attention of many rows over the paged cache: prompts, and blocks of more rows than k_paged_rows takes at once.
 //
 // A workgroup takes 128 rows of a request and KV head (its new tokens x the query heads that share the KV head), 32 per wave; keys
-// and values pass through LDS in blocks of 64 positions, a ring of them, loaded straight from the pages (global_load_lds, 16 bytes
-// a lane; a wave fetches the keys and the values of the same sixteen positions, which lie in one page).  On 32x32x16 products:
+// and values pass through LDS in blocks of 64 positions (float: 32), a ring of them, loaded straight from the pages (global_load_lds,
+// 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in one page).  On 32x32x16
+// products of bf16:
 //   S^T = K Q^T    the A operand's rows are dealt (bits 2 and 3 of the row swapped) so that a lane's sixteen scores of a tile are
 //                  two runs of eight consecutive keys of one query ...
 //   O^T += V^T P^T ... which are, rounded to bf16, the B operand as they stand; the A operand is one 16-byte LDS read from the V
@@ -13,8 +14,10 @@
 // rescaling the outputs is rare.
 // Probabilities enter the product as one bf16 term, an error of at most 2^-8 relative each, in the mean like that of the output's own
 // rounding: the error against 64 bits is 1.1 to 1.35 times that of a result rounded once.  Two terms cost 478 -> 600 us (below).
+// Float multiplies by 32x32x2 products: a lane's sixteen scores of a tile are four runs of four keys, in the order of the B operand's
+// halves, and the probabilities enter as they are.
 //
-// Bound by the matrix cores and the vector unit, which a SIMD's two waves, of different workgroups, overlap: the waves of one workgroup
+// bf16 is bound by the matrix cores and the vector unit, which a SIMD's two waves, of different workgroups, overlap: the waves of one workgroup
 // run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 467 = 1.03 PFLOP/s, of
 // 64 (241 GFLOP) 292, 16 / 8 of 256 (481 GFLOP) 679; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 188: a cap is two
 // transcendentals a score more.  With up to 32 rows per request it is bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16
@@ -23,16 +26,21 @@
 // Two workgroups of four waves against one of eight with the keys loaded half as often: 503 and 499 us for the prompts above, six of up
 // to 777 behind 900, 28 / 4 heads of 64, with a bias 53 and 72.  Priority to the phases of products: 481 -> 460, one of 723 behind 20990,
 // 56 / 8 of 64, with a cap 464 -> 436.  The next block's scores beside this block's exponentials in one wave, blocks of 32: 655 -> 735.
+// Float is bound by the matrix cores, whose 64 cycles a product hide the rest: one prompt of 2048 behind 20000, 8 / 2 heads of 128 (176
+// GFLOP) 1357 us = 130 TFLOP/s (k_paged_rows 1707; a library's product of 8192^3 153).
 #include "paged.h"
 
 namespace wisv {
 
 typedef float paged_f16 __attribute__((ext_vector_type(16)));
 typedef __bf16 paged_bf16x2 __attribute__((ext_vector_type(2)));
-constexpr int BLOCK = 64;   // positions
+template <typename T> constexpr int BLOCK = 128 / (int)sizeof(T);   // positions: 64, float 32
 
 __device__ __forceinline__ paged_f16 mfma32(paged_u4 a, paged_u4 b, paged_f16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<paged_bf16x8 *>(&a), *reinterpret_cast<paged_bf16x8 *>(&b), c, 0, 0, 0);
+}
+__device__ __forceinline__ paged_f16 mfma32(uint32_t a, uint32_t b, paged_f16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
 }
 // lane l: 16 bytes from base + voff to lds_addr + 16 l
 __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, const void *base) {
@@ -42,16 +50,18 @@ __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, co
 constexpr int PROMPT_WAVES = 4;
 // Blocks in LDS, 64 KB or (head_dim 256, whose registers allow one workgroup per CU) 128; rings of twice as many were no faster
 constexpr int prompt_stages(int hd) { return hd == 256 ? 2 : 256 / hd; }
-constexpr size_t prompt_lds(int hd) { return (size_t)prompt_stages(hd) * 2 * BLOCK * hd * 2; }
+constexpr size_t prompt_lds(int hd) { return (size_t)prompt_stages(hd) * 2 * 128 * hd; }
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 
-template <int HD, int MODS>
+template <typename T, int HD, int MODS>
 __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_prompt(PagedAttn a) {
     extern __shared__ __align__(16) unsigned char lds[];   // [STAGES][K, V][BLOCK * HD]
-    constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / 8, QT = HD / 16, OT = HD / 32, STAGES = prompt_stages(HD);
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int BLOCK = wisv::BLOCK<T>, RUNS = BLOCK / 16, TILES = BLOCK / 32, PER = 16 / (int)sizeof(T);   // PER: elements in 16 bytes
+    constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / PER, QT = CPR / 2, OT = HD / 32, STAGES = prompt_stages(HD);
     constexpr float LOG2E = 1.4426950408889634f;
-    constexpr int HALF = BLOCK * HD * 2, BUF = 2 * HALF;               // bytes
-    constexpr int LOADS = HD / 32, WAITS = 2 * LOADS;                  // loads of 1 KB that sixteen positions take of either pool, and of both
+    constexpr int HALF = 128 * HD, BUF = 2 * HALF;                     // bytes
+    constexpr int OWN = BLOCK / PROMPT_WAVES, LOADS = HD / 32, WAITS = 2 * LOADS;   // positions a wave fetches, in loads of 1 KB of either pool, and of both
     static_assert(STAGES >= 2 && (STAGES - 2) * WAITS <= 63, "vmcnt holds six bits");
     const int tid = threadIdx.x, lane = tid & 63, h2 = lane >> 5, qi = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -76,11 +86,11 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
     const int rho = min(wrow + qi, R - 1), tok = rho / a.rep, head = g * a.rep + rho % a.rep, pos = rq.pos0 + tok;
     const int lo = a.window ? pos - a.window : -1;   // the position before the window
     const float slope = (MODS & BIAS) && a.slopes ? a.slopes[head] * LOG2E : 0.f;
-    paged_u4 q[QT];   // lane: features 16 t + 8 h2 .. + 7 of its row
+    paged_u4 q[QT];   // lane: features PER (2 t + h2) .. of its row
     {
-        const bf16_t *src = (const bf16_t *)a.q + (int64_t)(rq.row0 + tok) * a.q_stride + (int64_t)head * HD + 8 * h2;
+        const T *src = (const T *)a.q + (int64_t)(rq.row0 + tok) * a.q_stride + (int64_t)head * HD + PER * h2;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) q[t] = *reinterpret_cast<const paged_u4 *>(src + 16 * t);
+        for (int t = 0; t < QT; ++t) q[t] = *reinterpret_cast<const paged_u4 *>(src + 2 * PER * t);
     }
 
     // ---- holes in the part of the table that this workgroup reads: then every block is looked at
@@ -91,33 +101,36 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
     }
     hole = __syncthreads_or(hole);
 
-    // ---- fetching: every wave fetches sixteen positions of a block, which lie in one page, of both pools.  Chunk c of key row r
+    // ---- fetching: every wave fetches OWN positions of a block, which lie in one page, of both pools.  Chunk c of key row r
     //      lies at chunk c ^ swizzle(r) in LDS, the values as they lie in the pool
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * 16 * HD * 2;
-    constexpr int SWZ_SHIFT = CPR == 4 ? 2 : CPR == 8 ? 1 : 0, SWZ_MASK = CPR == 32 ? 15 : CPR - 1;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * OWN * HD * (int)sizeof(T);
+    constexpr int SWZ_SHIFT = CPR == 4 ? 2 : CPR == 8 ? 1 : 0, SWZ_MASK = CPR >= 16 ? 15 : CPR - 1;
     uint32_t koff[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int r = i * (512 / HD) + lane / CPR;
-        koff[i] = r * HD * 2 + ((lane % CPR) ^ ((r >> SWZ_SHIFT) & SWZ_MASK)) * 16;
+        const int r = i * (64 / CPR) + lane / CPR;
+        koff[i] = r * CPR * 16 + ((lane % CPR) ^ (((wave * OWN + r) >> SWZ_SHIFT) & SWZ_MASK)) * 16;
     }
     const auto place = [&](int step) {   // elements from a pool's start to this wave's positions
-        const int key = step * BLOCK + 16 * wave;
+        const int key = step * BLOCK + OWN * wave;
         const int id = table[min(key >> a.page_shift, a.max_pages - 1)];
         return (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.page_stride + (((int64_t)g << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * HD;
     };
     const auto fetch = [&](int64_t at, int stage) __attribute__((always_inline)) {
         const uint32_t to = lds0 + stage * BUF;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) page_to_lds(to + i * 1024, koff[i], (const bf16_t *)a.k_pages + at);
+        for (int i = 0; i < LOADS; ++i) page_to_lds(to + i * 1024, koff[i], (const T *)a.k_pages + at);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) page_to_lds(to + HALF + i * 1024, i * 1024 + lane * 16, (const bf16_t *)a.v_pages + at);
+        for (int i = 0; i < LOADS; ++i) page_to_lds(to + HALF + i * 1024, i * 1024 + lane * 16, (const T *)a.v_pages + at);
     };
 
-    // ---- reading: K rows with bits 2 and 3 swapped, chunk 2 t + h2; V groups 2 kc + h2
-    const int krow = (qi & ~12) | ((qi & 4) << 1) | ((qi & 8) >> 1);
-    const uint32_t kaddr = krow * HD * 2 + ((h2 ^ ((krow >> SWZ_SHIFT) & SWZ_MASK)) * 16);   // of chunk h2; chunk 2 t + h2 lies at kaddr ^ 32 t
-    const uint32_t vaddr = HALF + (h2 * HD + qi) * 16;
+    // ---- reading: K rows (bf16: with bits 2 and 3 swapped), chunk 2 t + h2; of V the group of eight keys 2 kc + h2 (float: half h2
+    //      of a group, four keys).  Register r of tile i of the scores is then key 32 i + key_of(r) + first
+    const int krow = BF ? (qi & ~12) | ((qi & 4) << 1) | ((qi & 8) >> 1) : qi;
+    const uint32_t kaddr = krow * CPR * 16 + ((h2 ^ ((krow >> SWZ_SHIFT) & SWZ_MASK)) * 16);   // of chunk h2; chunk 2 t + h2 lies at kaddr ^ 32 t
+    const uint32_t vaddr = HALF + (BF ? (h2 * HD + qi) * 16 : qi * 32 + h2 * 16);
+    const auto key_of = [](int r) { return BF ? 16 * (r >> 3) + (r & 7) : 8 * (r >> 2) + (r & 3); };
+    const int first = (BF ? 8 : 4) * h2;
 
     // every row from position p0 to p1 sees every key of the block
     const auto see_all = [&](int key0, int p0, int p1) {
@@ -128,10 +141,10 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
         return !busy || (key0 >= rq.prefix && (key0 > pos_max || (a.window && key0 + BLOCK - 1 <= pos_min - a.window)));
     };
     const auto runs_there = [&](int key0) {   // bit i: run i of sixteen keys is in a page
-        uint32_t ok = 15;
+        uint32_t ok = (1u << RUNS) - 1;
         if (hole) {
             ok = 0;
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < RUNS; ++i) {
                 const int key = key0 + 16 * i;
                 if (key < rq.n_keys && (unsigned)table[key >> a.page_shift] < (unsigned)a.n_pages) ok |= 1u << i;
             }
@@ -147,7 +160,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     const float scale2 = a.scale * LOG2E;                                                   // scores in units of ln 2
-    const float cap_in = 2.f * scale2 / a.softcap, cap_out = a.softcap * LOG2E;             // (CAP only)
+    const float cap_in = (BF ? 2.f * scale2 : a.scale) / a.softcap, cap_out = a.softcap * LOG2E;             // (CAP only)
     const paged_f16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
     int64_t at_next = 0;   // where this wave's positions of the next block to be fetched lie
@@ -177,14 +190,15 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             // The same holds for values that only some rows see: those that are not finite are taken out and added at the end.
             const uint32_t ok = runs_there(key0);
             uint32_t out = 0;
-            for (int i = tid; i < BLOCK * HD / 8; i += 64 * PROMPT_WAVES) {
-                const int group = i / HD, n = ok >> (group >> 1) & 1 ? rq.n_keys - (key0 + 8 * group) : 0;   // of the group's eight keys
+            for (int i = tid; i < HALF / 16; i += 64 * PROMPT_WAVES) {
+                const int key = BF ? i / HD * 8 : i / (2 * HD) * 8 + (i & 1) * 4;            // the first of the chunk's PER keys
+                const int n = ok >> (key >> 4) & 1 ? rq.n_keys - (key0 + key) : 0;          // of them
                 paged_u4 *to = reinterpret_cast<paged_u4 *>(lds + stage * BUF + HALF) + i;
                 paged_u4 v = *to;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    v[w] &= (2 * w < n ? 0xffffu : 0u) | (2 * w + 1 < n ? 0xffff0000u : 0u);
-                    const uint32_t fine = finite_halves(v[w]);
+                    v[w] &= BF ? (2 * w < n ? 0xffffu : 0u) | (2 * w + 1 < n ? 0xffff0000u : 0u) : w < n ? 0xffffffffu : 0u;
+                    const uint32_t fine = BF ? finite_halves(v[w]) : (v[w] & 0x7f800000u) != 0x7f800000u ? 0xffffffffu : 0u;
                     out |= v[w] & ~fine;
                     v[w] &= fine;
                 }
@@ -193,25 +207,33 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             odd |= __syncthreads_or(out != 0);
         }
         if (see_none(key0)) continue;
-        // ---- scores: register r of tile i is key 32 i + 16 (r / 8) + 8 h2 + r % 8
-        paged_f16 x[2];
+        // ---- scores
+        paged_f16 x[TILES];
         __builtin_amdgcn_s_setprio(1);   // products first: the other workgroup's wave has its exponentials meanwhile
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                x[i] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + ((kaddr + stage * BUF) ^ (32 * t)) + i * 32 * HD * 2), q[t], t ? x[i] : zero);
+            for (int i = 0; i < TILES; ++i) {
+                const paged_u4 k = *reinterpret_cast<const paged_u4 *>(lds + ((kaddr + stage * BUF) ^ (32 * t)) + i * 32 * HD * (int)sizeof(T));
+                if constexpr (BF) {
+                    x[i] = mfma32(k, q[t], t ? x[i] : zero);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i] = mfma32(k[j], q[t][j], t || j ? x[i] : zero);
+                }
+            }
         __builtin_amdgcn_s_setprio(0);
         if (MODS != PLAIN) {   // into units of ln 2, with cap and bias (PLAIN scales them with the exponentials)
-            const float near = slope * (float)(key0 + 8 * h2 - pos);
+            const float near = slope * (float)(key0 + first - pos);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < TILES; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float bias = MODS & BIAS ? fmaf(slope, (float)(32 * i + 16 * (r >> 3) + (r & 7)), near) : 0.f;
+                    const float bias = MODS & BIAS ? fmaf(slope, (float)(32 * i + key_of(r)), near) : 0.f;
                     if (MODS & CAP) {
-                        const float t = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[i][r] * cap_in) + 1.f);   // tanh = 1 - 2 t
-                        x[i][r] = fmaf(t, -2.f * cap_out, cap_out + bias);
+                        // tanh = 1 - 2 / (exp(2 x) + 1)
+                        if (BF) x[i][r] = fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[i][r] * cap_in) + 1.f), -2.f * cap_out, cap_out + bias);
+                        else x[i][r] = fmaf(cap_out, tanhf(x[i][r] * cap_in), bias);
                     } else {
                         x[i][r] = fmaf(x[i][r], scale2, bias);
                     }
@@ -220,22 +242,24 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
         if (!see_all(key0, pos_min, pos_max)) {
             const uint32_t ok = runs_there(key0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < TILES; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int run = 2 * i + (r >> 3), j = key0 + 16 * run + 8 * h2 + (r & 7);
+                    const int run = 2 * i + (key_of(r) >> 4), j = key0 + 32 * i + key_of(r) + first;
                     x[i][r] = paged_sees(j, ok >> run & 1 ? rq.n_keys : 0, rq.prefix, pos, lo) ? x[i][r] : -INFINITY;
                 }
         }
         // (the maximum that lets NaN through is one instruction for two values; a row with one is NaN whatever the reference)
-        float part[4];
+        float part[2 * TILES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * TILES; ++i) {
             part[i] = x[i >> 1][8 * (i & 1)];
 #pragma unroll
             for (int r = 1; r < 8; ++r) part[i] = __builtin_elementwise_maximum(part[i], x[i >> 1][8 * (i & 1) + r]);
         }
-        float mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(part[0], part[1]), __builtin_elementwise_maximum(part[2], part[3]));
+        float mx = part[0];
+#pragma unroll
+        for (int i = 1; i < 2 * TILES; ++i) mx = __builtin_elementwise_maximum(mx, part[i]);
         const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);   // the lower and the upper lanes', in all
         mx = __builtin_elementwise_maximum(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
         if (MODS == PLAIN) mx *= scale2;
@@ -249,30 +273,47 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             for (int dt = 0; dt < OT; ++dt) o[dt] *= alpha;
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;   // a row that has seen no key yet
-        paged_u4 p[4];
-        const auto probs = [&](int kc) __attribute__((always_inline)) {
+        if constexpr (BF) {
+            paged_u4 p[4];
+            const auto probs = [&](int kc) __attribute__((always_inline)) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float x0 = x[kc >> 1][8 * (kc & 1) + 2 * w], x1 = x[kc >> 1][8 * (kc & 1) + 2 * w + 1];
-                const float e0 = __builtin_amdgcn_exp2f(MODS ? x0 - sub : fmaf(x0, scale2, -sub)), e1 = __builtin_amdgcn_exp2f(MODS ? x1 - sub : fmaf(x1, scale2, -sub));
-                const uint32_t both = f32x2_to_bf16x2(e0, e1);
-                p[kc][w] = both;
-                // (the sum of what the product weighs with: rounding errors that all probabilities share cancel)
-                l_run[w & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(paged_bf16x2, both), __builtin_bit_cast(paged_bf16x2, 0x3f803f80u), l_run[w & 1], false);
-            }
-        };
-        // a run of sixteen keys' products, and the next run's exponentials beside them
-        probs(0);
-        __builtin_amdgcn_s_setprio(1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int kc = 0; kc < 4; ++kc) {
-#pragma unroll
-            for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
-            if (kc < 3) probs(kc + 1);
+                for (int w = 0; w < 4; ++w) {
+                    const float x0 = x[kc >> 1][8 * (kc & 1) + 2 * w], x1 = x[kc >> 1][8 * (kc & 1) + 2 * w + 1];
+                    const float e0 = __builtin_amdgcn_exp2f(MODS ? x0 - sub : fmaf(x0, scale2, -sub)), e1 = __builtin_amdgcn_exp2f(MODS ? x1 - sub : fmaf(x1, scale2, -sub));
+                    const uint32_t both = f32x2_to_bf16x2(e0, e1);
+                    p[kc][w] = both;
+                    // (the sum of what the product weighs with: rounding errors that all probabilities share cancel)
+                    l_run[w & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(paged_bf16x2, both), __builtin_bit_cast(paged_bf16x2, 0x3f803f80u), l_run[w & 1], false);
+                }
+            };
+            // a run of sixteen keys' products, and the next run's exponentials beside them
+            probs(0);
+            __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kc = 0; kc < 4; ++kc) {
+#pragma unroll
+                for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
+                if (kc < 3) probs(kc + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+        } else {
+            // (exact in float; the products are 25 times the exponentials)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[0][r] = __builtin_amdgcn_exp2f(MODS ? x[0][r] - sub : fmaf(x[0][r], scale2, -sub));
+                l_run[r & 1] += x[0][r];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int dt = 0; dt < OT; ++dt) {
+                    const paged_u4 v = *reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (i * HD + 32 * dt) * 32);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[dt] = mfma32(v[j], __float_as_uint(x[0][4 * i + j]), o[dt]);
+                }
         }
-        __builtin_amdgcn_s_setprio(0);
     }
 
     if (odd) {
@@ -285,7 +326,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             for (int j = key0; j < min(key0 + BLOCK, rq.n_keys); ++j) {
                 const int id = table[j >> a.page_shift], in = j & ((1 << a.page_shift) - 1);
                 if ((unsigned)id >= (unsigned)a.n_pages || !paged_sees(j, rq.n_keys, rq.prefix, pos, lo)) continue;
-                const bf16_t *v = (const bf16_t *)a.v_pages + (int64_t)id * a.page_stride + (((int64_t)g << a.page_shift) + (in & ~7)) * HD + (in & 7) + 32 * h2;
+                const T *v = (const T *)a.v_pages + (int64_t)id * a.page_stride + (((int64_t)g << a.page_shift) + (in & ~7)) * HD + (in & 7) + 32 * h2;
 #pragma unroll
                 for (int dt = 0; dt < OT; ++dt)
 #pragma unroll
@@ -300,13 +341,15 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
     const int64_t row = rq.row0 + tok;
     if (a.n_splits == 1) {
         const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees no key is 0
-        bf16_t *dst = (bf16_t *)a.out + row * a.out_stride + (int64_t)head * HD + 4 * h2;
+        T *dst = (T *)a.out + row * a.out_stride + (int64_t)head * HD + 4 * h2;
 #pragma unroll
         for (int dt = 0; dt < OT; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<uint2 *>(dst + 32 * dt + 8 * i) = make_uint2(f32x2_to_bf16x2(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
-                                                                                f32x2_to_bf16x2(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
+            for (int i = 0; i < 4; ++i) {
+                const paged_f4 v = paged_f4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]} * inv;
+                if (BF) *reinterpret_cast<uint2 *>(dst + 32 * dt + 8 * i) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+                else *reinterpret_cast<paged_f4 *>(dst + 32 * dt + 8 * i) = v;
+            }
     } else {
         const int64_t to = ((int64_t)split * a.n_tokens + row) * a.H + head;
         if (l != 0.f) {   // (a part without keys is not read)
@@ -325,32 +368,37 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
 
 int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
-template <int HD, int MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
+template <typename T, int HD, int MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
     static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
     const size_t lds = prompt_lds(HD);
     if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
             (void)hipGetLastError();
             return "the device refuses the kernel's LDS request";
         }
         if (device >= 0 && device < MAX_DEVICES) allowed[device] = true;
     }
-    hipLaunchKernelGGL((k_paged_prompt<HD, MODS>), dim3(paged_prompt_tiles(a) * a.G, a.n_splits), dim3(64 * PROMPT_WAVES), lds, stream, a);
+    hipLaunchKernelGGL((k_paged_prompt<T, HD, MODS>), dim3(paged_prompt_tiles(a) * a.G, a.n_splits), dim3(64 * PROMPT_WAVES), lds, stream, a);
     return nullptr;
 }
-template <int HD> static const char *launch_m(const PagedAttn &a, int device, hipStream_t stream) {
+template <typename T, int HD> static const char *launch_m(const PagedAttn &a, int device, hipStream_t stream) {
     const bool cap = a.softcap > 0.f;
     // (PLAIN scales the maximum in the place of the scores, which only a positive scale keeps a maximum)
-    if (a.slopes || (a.scale < 0.f && !cap)) return cap ? launch_t<HD, CAP | BIAS>(a, device, stream) : launch_t<HD, BIAS>(a, device, stream);
-    return cap ? launch_t<HD, CAP>(a, device, stream) : launch_t<HD, PLAIN>(a, device, stream);
+    if (a.slopes || (a.scale < 0.f && !cap)) return cap ? launch_t<T, HD, CAP | BIAS>(a, device, stream) : launch_t<T, HD, BIAS>(a, device, stream);
+    return cap ? launch_t<T, HD, CAP>(a, device, stream) : launch_t<T, HD, PLAIN>(a, device, stream);
 }
-const char *launch_paged_prompt(const PagedAttn &a, int head_dim, int device, hipStream_t stream) {
+template <typename T> static const char *launch_d(const PagedAttn &a, int head_dim, int device, hipStream_t stream) {
     switch (head_dim) {
-        case 32: return launch_m<32>(a, device, stream);
-        case 64: return launch_m<64>(a, device, stream);
-        case 128: return launch_m<128>(a, device, stream);
-        default: return launch_m<256>(a, device, stream);
+        case 32:
+            if constexpr (sizeof(T) == 2) return launch_m<T, 32>(a, device, stream);   // (float, head_dim 32: k_paged_rows, by paged_cut)
+            return "no such kernel";
+        case 64: return launch_m<T, 64>(a, device, stream);
+        case 128: return launch_m<T, 128>(a, device, stream);
+        default: return launch_m<T, 256>(a, device, stream);
     }
+}
+const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, int device, hipStream_t stream) {
+    return bf16 ? launch_d<bf16_t>(a, head_dim, device, stream) : launch_d<float>(a, head_dim, device, stream);
 }
 
 }  // namespace wisv

@@ -44,9 +44,9 @@ struct PagedCut {
     size_t workspace;              // bytes
 };
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len);
-// The kernel of many rows (bf16), and how many tiles a call has at most
+// The kernel of many rows, and how many tiles a call has at most
 int paged_prompt_tiles(const PagedAttn &a);
-const char *launch_paged_prompt(const PagedAttn &a, int head_dim, int device, hipStream_t stream);
+const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, int device, hipStream_t stream);
 // null, or why the launch failed
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream);
 

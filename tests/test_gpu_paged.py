@@ -650,3 +650,64 @@ def test_append_of_two_rows_with_one_slot_leaves_either(ctx, dtype):
     assert (k == kp[1, :, 5]).any(0).all() and (v == vp[1, :, 0, :, 5]).any(0).all()
     kp[1, :, 5], vp[1, :, 0, :, 5] = before[0][1, :, 5], before[1][1, :, 0, :, 5]
     assert torch.equal(kp, before[0]) and torch.equal(vp, before[1])
+
+
+# ------------------------------------------------------------------------------------------------ float prompts of many rows
+
+# (128 or more tiles of 128 rows, at most a quarter of them empty: float calls that reach the kernel of many rows)
+FLOAT_PROMPTS = [(128, 32, 16, [290, 260, 512, 256], [256, 256, 230, 256]), (64, 44, 44, [130, 128, 77, 140], [128, 128, 77, 120]),
+                 (256, 16, 8, [600, 640], [600, 550]), (64, 64, 8, [300], [290])]
+
+
+@pytest.mark.parametrize("dim,h,g,lens,news", FLOAT_PROMPTS)
+@pytest.mark.parametrize("mods", [{}] + MODS, ids=lambda m: "-".join(m) or "plain")
+def test_attention_of_float_prompts(ctx, dim, h, g, lens, news, mods):
+    kw = dict(mods)
+    if kw.pop("slopes", False):
+        kw["slopes"] = 2.0 ** (-8.0 * np.arange(1, h + 1) / h)
+    if kw.pop("prefix", False):
+        kw["prefix"] = [5, 64, 3, 90][:len(lens)]
+    q, kp, vp, table, starts = setup(F32, dim, h, g, 16, lens, news, seed=5)
+    check_attention(ctx, q, kp, vp, table, starts, lens, **kw)
+
+
+def test_attention_of_float_prompts_cut_along_the_keys(ctx):
+    lens, news = [2900], [520]
+    q, kp, vp, table, starts = setup(F32, 64, 32, 4, 64, lens, news, seed=6)
+    check_attention(ctx, q, kp, vp, table, starts, lens)
+    check_attention(ctx, q, kp, vp, table, starts, lens, window=300, prefix=[70])
+
+
+def test_float_prompts_read_nothing_that_they_should_not(ctx):
+    """Holes, page ends and spare pages full of NaN; values that are not finite in the places of some rows."""
+    lens, news, page, h, g = [290, 270], [256, 250], 16, 64, 32
+    q, kp, vp, table, starts = setup(F32, 64, h, g, page, lens, news, seed=8)
+    table[0, 2], table[1, 4], table[1, 9] = -1, 10 ** 6, -7
+    clean, _ = check_attention(ctx, q, kp, vp, table, starts, lens)
+    held = np.zeros((kp.shape[0], page), bool)
+    for b, n in enumerate(lens):
+        for j in range(n):
+            if 0 <= table[b, j // page] < kp.shape[0]:
+                held[table[b, j // page], j % page] = True
+    bad = torch.from_numpy(~held).to(DEV)
+    kp2 = torch.where(bad[:, None, :, None], torch.full_like(kp, float("nan")), kp)
+    vp2 = torch.where(bad.view(kp.shape[0], 1, page // 8, 1, 8), torch.full_like(vp, float("inf")), vp)
+    args = (ints(table), ints(starts), ints(lens))
+    assert torch.equal(clean, ctx.wisv_paged_attention(q, kp2, vp2, *args, max_new=max(news), max_len=max(lens)))
+    at, feature = 200, 37
+    vp2[int(table[0, at // page]), :, (at % page) // 8, feature, at % 8] = float("nan")
+    got = ctx.wisv_paged_attention(q, kp2, vp2, *args, max_new=max(news), max_len=max(lens))
+    sees = torch.zeros_like(got, dtype=torch.bool)
+    sees[at - (lens[0] - news[0]):news[0], :, feature] = True
+    assert torch.equal(got.isnan(), sees) and torch.equal(got[~sees], clean[~sees])
+
+
+def test_float_prompts_with_strides_and_padding_rows(ctx):
+    lens, news, h, dim = [300], [280], 64, 64
+    q, kp, vp, table, starts = setup(F32, dim, h, 8, 32, lens, news, seed=9, spare_rows=40)
+    wide = torch.full((q.shape[0], h * dim + 36), float("nan"), dtype=F32, device=DEV)
+    wide[:, :h * dim] = q.reshape(q.shape[0], -1)
+    out = torch.full((q.shape[0], h * dim + 20), 3.0, dtype=F32, device=DEV)
+    view = out[:, :h * dim].view(-1, h, dim)
+    check_attention(ctx, wide[:, :h * dim].view(-1, h, dim), kp, vp, table, starts, lens, out=view)
+    assert (out[:, h * dim:] == 3.0).all() and (view[280:] == 3.0).all()

@@ -216,3 +216,22 @@ def test_which_kernel_serves_which_rows(stub):
         long = dict(batch=1, max_pages=4096, max_len=65536)
         assert served(n_tokens=1, max_new=1, **long) == "rj" and served(n_tokens=40, max_new=40, **long) == "pj"
     ''')
+
+
+def test_which_kernel_serves_float_prompts(stub):
+    run(stub, '''
+        def served(**kw):
+            stub.stub_log_clear()
+            need_ = need(dtype=0, **kw)
+            assert attn(dtype=0, **kw, workspace=P if need_ else None, workspace_bytes=need_) == 0, text()
+            return "".join("p" if "prompt" in l else "j" if "join" in l else "r" if "rows" in l else "?" for l in log())
+        # two rows per token, two KV heads: 128 tiles from 4096 tokens on
+        assert served(n_tokens=4096, max_new=2048) == "p" and served(n_tokens=4032, max_new=2048) == "r"
+        for batch, kernel in ((64, "p"), (85, "p"), (90, "r")):     # 128, 97 and 92 of a tile's rows
+            assert served(n_tokens=4096 if batch == 64 else 48 * 85 + 49 if batch == 85 else 46 * 90, max_new=64, batch=batch) == kernel, batch
+        assert served(n_tokens=4096, max_new=2048, head_dim=32, q_stride=128, out_stride=128) == "r"
+        assert served(n_tokens=4096, max_new=2048, head_dim=256, q_stride=1024, out_stride=1024) == "p"
+        stub.stub_refuse_lds(1)
+        assert attn(dtype=0, n_tokens=4096, max_new=2048, head_dim=128, q_stride=512, out_stride=512) == B.WISV_EHIP and "LDS" in text()
+        stub.stub_refuse_lds(0)
+    ''')
