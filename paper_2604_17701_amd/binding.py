@@ -193,6 +193,8 @@ def paged_fill(k_pages: torch.Tensor, v_pages: torch.Tensor, pages: Sequence[int
     """Writes k, v ([n_kv_heads, len, head_dim], positions 0..len-1) into the pages of one request, in order."""
     g, n, hd = k.shape
     ps = k_pages.shape[2]
+    if len(pages) * ps < n:
+        raise ValueError(f"{len(pages)} pages of {ps} do not hold {n} positions")
     for i, page in enumerate(pages[:(n + ps - 1) // ps]):
         m = min(ps, n - i * ps)
         k_pages[page, :, :m] = k[:, i * ps:i * ps + m]
@@ -410,7 +412,8 @@ class Context:
         if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
             if n > 1:
                 stride = k_pages.stride(0)
-            if (n > 1 and v_pages.stride(0) != stride) or not (k_pages[:1].is_contiguous() and v_pages[:1].is_contiguous()):
+            if stride < g * ps * hd or (n > 1 and v_pages.stride(0) != stride) \
+                    or not (k_pages[:1].is_contiguous() and v_pages[:1].is_contiguous()):
                 raise ValueError("a page must lie in one piece, and both pools must have the same distance from page to page")
         return n, g, ps, hd, WISV_BF16 if dt is torch.bfloat16 else WISV_F32, stride
 
@@ -422,8 +425,8 @@ class Context:
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
         width = block_table.shape[1]
-        if max_tokens < 1:
-            raise ValueError("max_tokens must be positive")
+        if not (0 < max_tokens < 1 << 31 and 0 < page_size < 1 << 31):
+            raise ValueError("max_tokens and page_size must be positive and fit 32 bits")
         sizes = (b + 1, b, max_tokens, max_tokens, 1, b)
         if out is None:
             buf = torch.empty(3 * b + 2 + 2 * max_tokens, dtype=torch.int32, device=self.device)
@@ -506,6 +509,10 @@ class Context:
                 raise ValueError("out must have the heads of q")
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
+        if not (abs(max_new) < 1 << 31 and abs(max_len) < 1 << 31 and abs(window) < 1 << 31):
+            raise ValueError("max_new, max_len and window must fit 32 bits")
+        if 0 < abs(scale) < 1e-37 or 0 < softcap < 1e-37:
+            raise ValueError("scale or softcap is 0 as a float32, which means something else")
         b, width = kv_len.numel(), block_table.shape[1]
         args = wisv_paged_attention_args(
             b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,

@@ -235,3 +235,46 @@ def test_which_kernel_serves_float_prompts(stub):
         assert attn(dtype=0, n_tokens=4096, max_new=2048, head_dim=128, q_stride=512, out_stride=512) == B.WISV_EHIP and "LDS" in text()
         stub.stub_refuse_lds(0)
     ''')
+
+
+class OnHost:
+    """Stands for a ctx whose tensors lie on the host (get_device() -1): the binding's checks alone."""
+    device = type("Device", (), {"index": -1})()
+
+    def __getattr__(self, name):
+        return getattr(binding.Context, name).__get__(self)
+
+
+def test_the_binding_refuses_pools_whose_pages_overlap():
+    k, v = binding.new_paged_cache(1, 2, 16, 64, torch.float32, "cpu")
+    spread = binding.new_paged_cache(3, 4, 16, 64, torch.float32, "cpu")
+    assert OnHost()._pools(k, v) == (1, 2, 16, 64, binding.WISV_F32, 2 * 16 * 64)
+    assert OnHost()._pools(spread[0][:, :2], spread[1][:, :2]) == (3, 2, 16, 64, binding.WISV_F32, 4 * 16 * 64)
+    one = (k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1, -1))       # one page three times: no distance, which would mean the usual one
+    near = (spread[0].as_strided((3, 2, 16, 64), (1024, 1024, 64, 1)), spread[1].as_strided((3, 2, 2, 64, 8), (1024, 1024, 512, 8, 1)))
+    for pools in (one, near):
+        with pytest.raises(ValueError, match="distance"):
+            OnHost()._pools(*pools)
+
+
+def test_the_binding_refuses_numbers_that_would_wrap():
+    k, v = binding.new_paged_cache(2, 1, 16, 32, torch.float32, "cpu")
+    ints = torch.zeros(1, dtype=torch.int32)
+    q, table = torch.zeros(1, 1, 32), torch.zeros((1, 2), dtype=torch.int32)
+    for kw, what in ((dict(window=1 << 32), "window"), (dict(window=-(1 << 32)), "window"), (dict(max_new=1 << 31), "max_new"), (dict(max_len=1 << 31), "max_len"),
+                     (dict(scale=1e-50), "scale"), (dict(scale=-1e-50), "scale"), (dict(softcap=1e-50), "softcap")):
+        with pytest.raises(ValueError, match=what):
+            OnHost().wisv_paged_attention(q, k, v, table, torch.zeros(2, dtype=torch.int32), ints, **kw)
+    for kw in (dict(page_size=16, max_tokens=0), dict(page_size=16, max_tokens=1 << 32), dict(page_size=(1 << 32) + 16, max_tokens=4)):
+        with pytest.raises(ValueError, match="max_tokens"):
+            OnHost().wisv_paged_plan(ints, ints, ints, table, **kw)
+
+
+def test_filling_needs_pages_for_every_position():
+    k, v = binding.new_paged_cache(4, 1, 16, 32, torch.float32, "cpu")
+    rows = torch.randn(1, 33, 32)
+    with pytest.raises(ValueError, match="hold"):
+        binding.paged_fill(k, v, [2, 0], rows, rows)
+    assert not k.any() and not v.any()
+    binding.paged_fill(k, v, [2, 0, 3], rows, rows)
+    assert torch.equal(torch.cat([k[2], k[0], k[3]], 1)[:, :33], rows)
