@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -104,6 +105,18 @@ class wisv_paged_attention_args(C.Structure):
                [("workspace_bytes", C.c_size_t), ("hip_stream", C.c_void_p)]
 
 
+def _packer(args):
+    """A function from the members of the C structure `args`, in order, to its bytes (0: a null pointer): a quarter of the time that
+    filling the structure takes, 0.6 us instead of 2.3 for wisv_paged_append's."""
+    codes = {C.c_int32: "i", C.c_int64: "q", C.c_float: "f", C.c_void_p: "P", C.c_size_t: "N"}
+    layout = struct.Struct("@" + "".join(codes[t] for _, t in args._fields_))
+    assert layout.size == C.sizeof(args)
+    return layout.pack
+
+
+_pack_plan, _pack_append, _pack_attention = (_packer(t) for t in (wisv_paged_plan_args, wisv_paged_append_args, wisv_paged_attention_args))
+
+
 class PagePlan(NamedTuple):
     """What wisv_paged_plan leaves (int32 device tensors; wisv.h says what they hold)."""
     q_start: torch.Tensor
@@ -147,10 +160,10 @@ def load_library() -> C.CDLL:
         lib.wisv_ss_decide_static.argtypes = lib.wisv_ss_decide.argtypes
         lib.wisv_set_option.argtypes = [C.c_void_p, C.c_int32, C.c_int64]
         lib.wisv_get_option.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_int64)]
-        lib.wisv_paged_plan.argtypes = [C.c_void_p, C.POINTER(wisv_paged_plan_args)]
-        lib.wisv_paged_append.argtypes = [C.c_void_p, C.POINTER(wisv_paged_append_args)]
-        lib.wisv_paged_attention_workspace.argtypes = [C.c_void_p, C.POINTER(wisv_paged_attention_args), C.POINTER(C.c_size_t)]
-        lib.wisv_paged_attention.argtypes = [C.c_void_p, C.POINTER(wisv_paged_attention_args)]
+        lib.wisv_paged_plan.argtypes = [C.c_void_p, C.c_void_p]   # (the paged operators' arguments are packed bytes)
+        lib.wisv_paged_append.argtypes = [C.c_void_p, C.c_void_p]
+        lib.wisv_paged_attention_workspace.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+        lib.wisv_paged_attention.argtypes = [C.c_void_p, C.c_void_p]
         lib.wisv_last_error.restype = C.c_char_p
         for name in EXPORTS:
             if name != "wisv_last_error":
@@ -439,10 +452,10 @@ class Context:
             ptrs = (p, kv, pos, slots, used, used + 4)
         else:
             ptrs = [self._ints(n, t, m) for n, t, m in zip(PagePlan._fields, out, sizes)]
-        args = wisv_paged_plan_args(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, b),
-                                    self._ints("new_len", new_len, b), self._ints("free_pages", free_pages, n_free) or None,
+        args = _pack_plan(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, b),
+                                    self._ints("new_len", new_len, b), self._ints("free_pages", free_pages, n_free),
                                     self._ints("block_table", block_table, b, width), *ptrs, self._stream_now())
-        rc = self._lib.wisv_paged_plan(self._h, C.byref(args))
+        rc = self._lib.wisv_paged_plan(self._h, args)
         if rc:
             self._check(rc)
         return out
@@ -459,8 +472,7 @@ class Context:
         vp, vg, vs = self._rows("v", v, dt, rows, hd)
         if kg != g or vg != g:
             raise ValueError(f"k and v must have the pools' {g} heads")
-        qp = qop = pp = cp = sp = None
-        heads = qs = qos = n_rope = 0
+        qp = qop = pp = cp = sp = heads = qs = qos = n_rope = 0
         if q is not None:
             qp, heads, qs = self._rows("q", q, dt, rows, hd)
             if q_out is None:
@@ -475,14 +487,14 @@ class Context:
         if positions is not None:
             pp = self._ints("positions", positions, rows)
         if cos is not None or sin is not None:
-            if cos is None or sin is None or pp is None or cos.dim() != 2:
+            if cos is None or sin is None or positions is None or cos.dim() != 2:
                 raise ValueError("cos and sin come together, [n_rope, head_dim / 2], and need positions")
             n_rope = cos.shape[0]
             cp, sp = self._floats("cos", cos, n_rope, hd >> 1), self._floats("sin", sin, n_rope, hd >> 1)
-        args = wisv_paged_append_args(rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos, pp,
+        args = _pack_append(rows, heads, g, hd, dtype, ps, n, n_rope, qp, kp, vp, qop, qs, ks, vs, qos, pp,
                                       self._ints("slots", slots, rows), cp, sp, k_pages.data_ptr(), v_pages.data_ptr(), stride,
                                       self._stream_now())
-        rc = self._lib.wisv_paged_append(self._h, C.byref(args))
+        rc = self._lib.wisv_paged_append(self._h, args)
         if rc:
             self._check(rc)
         return q_out
@@ -511,19 +523,19 @@ class Context:
             raise ValueError("block_table must be [batch, max_pages]")
         if not (abs(max_new) < 1 << 31 and abs(max_len) < 1 << 31 and abs(window) < 1 << 31):
             raise ValueError("max_new, max_len and window must fit 32 bits")
-        if 0 < abs(scale) < 1e-37 or 0 < softcap < 1e-37:
-            raise ValueError("scale or softcap is 0 as a float32, which means something else")
+        if 0 < abs(scale) < 1e-37 or 0 < softcap < 1e-37 or abs(scale) > 1e38 or softcap > 1e38:   # (0 means something else)
+            raise ValueError("scale and softcap must be float32 numbers")
         b, width = kv_len.numel(), block_table.shape[1]
-        args = wisv_paged_attention_args(
-            b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,
-            k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, b, width),
-            self._ints("q_start", q_start, b + 1), self._ints("kv_len", kv_len, b),
-            None if prefix_len is None else self._ints("prefix_len", prefix_len, b),
-            None if slopes is None else self._floats("slopes", slopes, heads), None, 0, self._stream_now())
-        ref = C.byref(args)
+        args = (b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,
+                k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, b, width),
+                self._ints("q_start", q_start, b + 1), self._ints("kv_len", kv_len, b),
+                0 if prefix_len is None else self._ints("prefix_len", prefix_len, b),
+                0 if slopes is None else self._floats("slopes", slopes, heads))
+        stream = self._stream_now()
         if workspace is None:
             need = C.c_size_t()
-            rc = self._lib.wisv_paged_attention_workspace(self._h, ref, C.byref(need))
+            packed = _pack_attention(*args, 0, 0, stream)
+            rc = self._lib.wisv_paged_attention_workspace(self._h, packed, C.byref(need))
             if rc:
                 self._check(rc)
             if need.value:
@@ -531,8 +543,8 @@ class Context:
         elif workspace.device != self.device or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {self.device}")
         if workspace is not None:
-            args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        rc = self._lib.wisv_paged_attention(self._h, ref)
+            packed = _pack_attention(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+        rc = self._lib.wisv_paged_attention(self._h, packed)
         if rc:
             self._check(rc)
         return out
