@@ -1,4 +1,4 @@
-// Attention of a chunk of new tokens over the paged cache: few rows per request (or float), the join of split keys, and the
+// Attention of a chunk of new tokens over the paged cache: few rows per request (or short float prompts), the join of split keys, and the
 // choice between this kernel and kernels_paged_prompt.hip's.
 //
 // k_paged_rows.  The rows of a request and KV head - its new tokens x the query heads that share the KV head, token by
@@ -15,8 +15,8 @@
 // Bound by bytes: 36 GB/s into one CU, about 6 TB/s into all; by latency below 100 KB per CU (a launch that reads next to nothing
 // takes 6.4 us), and float prompts by the float matrix rate.  Kernel traces: one token over 131072 positions, 32 / 8 heads of 128
 // (537 MB, 32 splits) 98 us = 5.5 TB/s; 36 tokens in windows of 4096, 16 / 8 heads of 256 (376 MB, ragged) 86 us = 4.4 TB/s; four
-// rows over 516 positions, 32 / 8 heads of 128 (2.2 MB, 4 splits) 8.7 us; a float prompt of 1024 behind 1024, 32 / 8 heads of 128,
-// 327 us = 79 TFLOP/s of 153.  Keys and values of one step in the same registers, so that two waves share a SIMD at head_dim
+// rows over 516 positions, 32 / 8 heads of 128 (2.2 MB, 4 splits) 8.7 us; 24 float requests of 40 tokens behind 4000, 32 / 8 heads of
+// 64 (32 GFLOP), 338 us = 94 TFLOP/s of 153.  Keys and values of one step in the same registers, so that two waves share a SIMD at head_dim
 // 256, spill (99 us -> 155).
 #include "paged.h"
 
@@ -449,18 +449,19 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     const int reach = a.window ? (int)std::min<int64_t>(max_len, (int64_t)a.window + 64 + (c.prompt ? 128 / a.rep : max_new)) : max_len;
     const int64_t steps = (reach + 63) / 64;
     if (c.prompt) {
-        // Workgroups run two to a CU (head_dim 256: one).  Splitting the keys fills a chip, or the last of its rounds, that is not
-        // full.  In steps of 64 keys, about 2 us each: a split costs six (its start, its way to the join), the join three and
-        // the parts' way through memory.  us per call: six prompts of up to 777 behind 900, 28 / 4 heads of 64, 1 split 43, 2 (taken)
-        // 38, 3 35, 4 42; one of 723 behind 20990, 56 / 8 of 64, 538, 562, 415, 4 (taken) 450; two of 2048 behind 6144, 32 / 8 of 128,
-        // 1 (taken) 472, 2 535
-        const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = head_dim == 256 ? 256 : 512;
+        // Splitting the keys fills a chip, or the last of its rounds, that is not full.  In steps of 64 keys, in bf16 about 2 us each: a
+        // split costs six (its start, its way to the join), the join three and the parts' way through memory; float steps are as much
+        // longer as its products.  us per call: six prompts of up to 777 behind 900, 28 / 4 heads of 64, with a bias 1 split 43, 2 36.7, 3
+        // 36.0, 4 36.2, the rule's 35.0; one of 723 behind 20990, 56 / 8 of 64, with a cap 548, 490, 437, 420, the rule's 481; two of 2048
+        // behind 6144, 32 / 8 of 128, 1 (taken) 482, 2 537; float, one of 2048 behind 20000, 8 / 2 of 128, with a cap 3417, 2636, 1993,
+        // 4 (taken) 1518, 6 1567
+        const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = 256 * paged_prompt_wgs(head_dim);
         const double fixed = bf16 ? 1 : 18.0 / head_dim;
         const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;
         double best = 0;
         c.n_splits = 1;
         for (int s = 1; s <= 32 && (s == 1 || steps / s >= 2); ++s) {
-            const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + 0.25) * ((double)steps / s + 6 * fixed) + (s > 1 ? (3 + s * part) * fixed : 0);
+            const double rounds = wgs * s / slots, cost = (rounds <= 1 ? 1 : rounds + (bf16 ? 0.25 : 0.5)) * ((double)steps / s + 6 * fixed) + (s > 1 ? (3 + s * part) * fixed : 0);
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     } else {
@@ -517,14 +518,14 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
     const PagedCut cut = paged_cut(a, bf16, head_dim, max_new, max_len);
     a.n_splits = cut.n_splits;
     if (cut.prompt) {
-        a.split_steps = cut.split_steps * (bf16 ? 1 : 2);
+        a.split_steps = cut.split_steps;
         if (const char *why = launch_paged_prompt(a, bf16, head_dim, device, stream)) return why;
     } else {
         a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
         const int64_t rows = (int64_t)a.rep * max_new;
         // Two query tiles per wave read the keys half as often; one where that leaves few workgroups (float, 5 requests of up to 37
         // rows, 4 KV heads: 15.8 us and 12.8) and at head_dim 256, where two do not fit the registers (float, 23 prompts of 400, one
-        // KV head: 785 us and 634)
+        // KV head, when this kernel served them: 785 us and 634)
         const bool two = rows > 16 && head_dim < 256 && ((int64_t)a.n_tokens * a.rep / 32 + 1) * a.G >= 32;
         a.tiles = rows > (two ? row_limit(bf16, head_dim) : 16);
         if (bf16) launch_rows_d<bf16_t>(a, head_dim, two, stream);

@@ -1,9 +1,9 @@
 // Attention of many rows over the paged cache: prompts, and blocks of more rows than k_paged_rows takes at once.
 //
 // A workgroup takes 128 rows of a request and KV head (its new tokens x the query heads that share the KV head), 32 per wave; keys
-// and values pass through LDS in blocks of 64 positions (float: 32), a ring of them, loaded straight from the pages (global_load_lds,
-// 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in one page).  On 32x32x16
-// products of bf16:
+// and values pass through LDS in blocks of 64 positions (float: 32), one read while the next arrives straight from the pages
+// (global_load_lds, 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in one page).
+// On 32x32x16 products of bf16:
 //   S^T = K Q^T    the A operand's rows are dealt (bits 2 and 3 of the row swapped) so that a lane's sixteen scores of a tile are
 //                  two runs of eight consecutive keys of one query ...
 //   O^T += V^T P^T ... which are, rounded to bf16, the B operand as they stand; the A operand is one 16-byte LDS read from the V
@@ -17,12 +17,16 @@
 // Float multiplies by 32x32x2 products: a lane's sixteen scores of a tile are four runs of four keys, in the order of the B operand's
 // halves, and the probabilities enter as they are.
 //
-// bf16 is bound by the matrix cores and the vector unit, which a SIMD's two waves, of different workgroups, overlap: the waves of one workgroup
-// run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 467 = 1.03 PFLOP/s, of
-// 64 (241 GFLOP) 292, 16 / 8 of 256 (481 GFLOP) 679; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 188: a cap is two
+// bf16 is bound by the matrix cores and the vector unit, which a SIMD's two or three waves, of different workgroups, overlap: the waves of one
+// workgroup run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 475 = 1.01 PFLOP/s, of
+// 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 662; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two
 // transcendentals a score more.  With up to 32 rows per request it is bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16
 // GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at head_dim 64, 1.4 at 128, 2.9 at 256, spread over loads, products,
 // exponentials and maxima.
+// Workgroups that share a CU count for more than blocks on their way: rings of 64 KB, for two workgroups, against these two blocks, for
+// three, the prompts above at head_dim 64 341 and 292, at 32 240 and 206.  At head_dim 128 three need blocks of 32 positions: 12 of 855
+// behind 187 164 and 156, but the prompts above 480 and 573, whose 1024 workgroups are no whole rounds of 768, and 64 of 32 over 8192
+// 403 and 440: two.
 // Two workgroups of four waves against one of eight with the keys loaded half as often: 503 and 499 us for the prompts above, six of up
 // to 777 behind 900, 28 / 4 heads of 64, with a bias 53 and 72.  Priority to the phases of products: 481 -> 460, one of 723 behind 20990,
 // 56 / 8 of 64, with a cap 464 -> 436.  The next block's scores beside this block's exponentials in one wave, blocks of 32: 655 -> 735.
@@ -48,21 +52,19 @@ __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, co
 }
 
 constexpr int PROMPT_WAVES = 4;
-// Blocks in LDS, 64 KB or (head_dim 256, whose registers allow one workgroup per CU) 128; rings of twice as many were no faster
-constexpr int prompt_stages(int hd) { return hd == 256 ? 2 : 256 / hd; }
-constexpr size_t prompt_lds(int hd) { return (size_t)prompt_stages(hd) * 2 * 128 * hd; }
+constexpr int prompt_lds(int hd) { return 4 * 128 * hd; }   // two blocks of keys and of values
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 
 template <typename T, int HD, int MODS>
-__global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_prompt(PagedAttn a) {
-    extern __shared__ __align__(16) unsigned char lds[];   // [STAGES][K, V][BLOCK * HD]
+__global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(HD)) void k_paged_prompt(PagedAttn a) {
+    extern __shared__ __align__(16) unsigned char lds[];   // [2][K, V][BLOCK * HD]
     constexpr bool BF = sizeof(T) == 2;
     constexpr int BLOCK = wisv::BLOCK<T>, RUNS = BLOCK / 16, TILES = BLOCK / 32, PER = 16 / (int)sizeof(T);   // PER: elements in 16 bytes
-    constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / PER, QT = CPR / 2, OT = HD / 32, STAGES = prompt_stages(HD);
+    constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / PER, QT = CPR / 2, OT = HD / 32;
     constexpr float LOG2E = 1.4426950408889634f;
-    constexpr int HALF = 128 * HD, BUF = 2 * HALF;                     // bytes
-    constexpr int OWN = BLOCK / PROMPT_WAVES, LOADS = HD / 32, WAITS = 2 * LOADS;   // positions a wave fetches, in loads of 1 KB of either pool, and of both
-    static_assert(STAGES >= 2 && (STAGES - 2) * WAITS <= 63, "vmcnt holds six bits");
+    constexpr int HALF = BLOCK * HD * (int)sizeof(T), BUF = 2 * HALF;   // bytes
+    constexpr int OWN = BLOCK / PROMPT_WAVES, LOADS = OWN * CPR / 64;   // positions a wave fetches, in loads of 1 KB of either pool
+    static_assert(LOADS * 64 == OWN * CPR, "whole loads");
     const int tid = threadIdx.x, lane = tid & 63, h2 = lane >> 5, qi = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = blockIdx.x % a.G, split = blockIdx.y;
@@ -165,25 +167,16 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
 
     int64_t at_next = 0;   // where this wave's positions of the next block to be fetched lie
     if (s_begin < s_end) {
-        int64_t at[STAGES - 1];
-#pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i) at[i] = place(real(min(s_begin + i, s_end - 1)));
-        at_next = place(real(min(s_begin + STAGES - 1, s_end - 1)));
-#pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i)
-            if (s_begin + i < s_end) fetch(at[i], i);
+        fetch(place(real(s_begin)), 0);
+        at_next = place(real(min(s_begin + 1, s_end - 1)));
     }
     for (int s = s_begin; s < s_end; ++s) {
-        // block s has arrived, everybody's part of it, and nobody reads block s - 1 any more; its place takes block s - 1 + STAGES
-        constexpr int MOST = STAGES - 2, SOME = MOST / 3;   // blocks that may still be on their way, where there are so many
-        const int left = s_end - s - 1;
-        if (left >= MOST) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(MOST * WAITS) : "memory");
-        else if (left >= SOME) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SOME * WAITS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int stage = (s - s_begin) % STAGES, key0 = real(s) * BLOCK;
-        if (s + STAGES - 1 < s_end) {
-            fetch(at_next, (stage + STAGES - 1) % STAGES);
-            at_next = place(real(min(s + STAGES, s_end - 1)));
+        // block s has arrived, everybody's part of it, and nobody reads block s - 1 any more; its place takes block s + 1
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int stage = (s - s_begin) & 1, key0 = real(s) * BLOCK;
+        if (s + 1 < s_end) {
+            fetch(at_next, stage ^ 1);
+            at_next = place(real(min(s + 2, s_end - 1)));
         }
         if (!see_all(key0, tile_min, tile_max)) {
             // values behind the end of the request, or of a page that is not there, may be anything: 0 x NaN would reach every row.
@@ -274,7 +267,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;   // a row that has seen no key yet
         if constexpr (BF) {
-            paged_u4 p[4];
+            paged_u4 p[RUNS];
             const auto probs = [&](int kc) __attribute__((always_inline)) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -291,10 +284,10 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
             __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int kc = 0; kc < 4; ++kc) {
+            for (int kc = 0; kc < RUNS; ++kc) {
 #pragma unroll
                 for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
-                if (kc < 3) probs(kc + 1);
+                if (kc < RUNS - 1) probs(kc + 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
             __builtin_amdgcn_s_setprio(0);
@@ -368,11 +361,12 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, HD == 256 ? 1 : 2) void k_paged_
 
 int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
-template <typename T, int HD, int MODS> static const char *launch_t(const PagedAttn &a, int device, hipStream_t stream) {
+template <typename T, int HD, int MODS> static const char *launch_t(PagedAttn a, int device, hipStream_t stream) {
+    a.split_steps *= 64 / BLOCK<T>;
     static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
-    const size_t lds = prompt_lds(HD);
+    constexpr int lds = prompt_lds(HD);
     if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
             (void)hipGetLastError();
             return "the device refuses the kernel's LDS request";
         }
