@@ -389,7 +389,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
         }
         float top = mx;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, l[i] != 0.f ? m[i] : -INFINITY);
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, l[i] != 0.f ? fmaxf(m[i], -3e38f) : -INFINITY);   // (scores that are all no numbers: -infinity)
         if (top == -INFINITY) continue;
         const float keep = __builtin_amdgcn_exp2f(mx - top);
         den *= keep;

@@ -711,3 +711,16 @@ def test_float_prompts_with_strides_and_padding_rows(ctx):
     view = out[:, :h * dim].view(-1, h, dim)
     check_attention(ctx, wide[:, :h * dim].view(-1, h, dim), kp, vp, table, starts, lens, out=view)
     assert (out[:, h * dim:] == 3.0).all() and (view[280:] == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, 2), (BF16, 40), (F32, 2), (F32, 40)])
+def test_attention_of_queries_that_are_no_numbers_over_cut_keys(ctx, dtype, new):
+    """Every part of the keys has nothing but NaN scores for such a row: it stays NaN, and no other row changes."""
+    lens, h = [4000], 4
+    q, kp, vp, table, starts = setup(dtype, 64, h, 2, 64, lens, [new])
+    clean, _ = check_attention(ctx, q, kp, vp, table, starts, lens)
+    q[1, 3, 7] = float("nan")
+    got = ctx.wisv_paged_attention(q, kp, vp, ints(table), ints(starts), ints(lens), new, 4000)
+    assert got[1, 3].isnan().all()
+    got[1, 3] = clean[1, 3]
+    assert torch.equal(got, clean)
