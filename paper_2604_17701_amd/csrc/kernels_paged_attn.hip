@@ -428,11 +428,12 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
 
 // ------------------------------------------------------------------------------------------ launch
 
-// Rows of a request that k_paged_rows takes: beyond them it would read the keys twice, and k_paged_prompt, which holds
-// 128, serves bf16.  At head_dim 128 that kernel is as fast from 17 rows on: 64 requests of 32 rows over 8192 positions 361 us, two
-// tiles of 16 here 370, 16 requests of 24 rows over 2048 30.1 and 30.7 (head_dim 64, 256 requests of 32 rows over 2048 235 and 205;
-// 256, 64 over 4096 446 and 390).
-static int row_limit(bool bf16, int head_dim) { return bf16 && head_dim == 128 ? 16 : 32; }
+// Rows of a request that k_paged_rows takes: beyond them it would read the keys twice, and k_paged_prompt, which holds 128, serves
+// bf16.  From head_dim 128 on, where its two query tiles do not fit the registers, that kernel is as fast or faster from 17 rows on.  us
+// per call, k_paged_rows and k_paged_prompt: 64 requests of 32 rows, over 8192 positions, head_dim 128, two tiles of 16, 370 and 361; over
+// 4096, 256, 441 and 365; over 512, 256, 89 and 51; over 8192, 64, 187 and 213; 256 of them over 2048, 64, 221 and 204; 64 of 16 rows over
+// 4096, 256, 366 and 361; 37 of two rows over up to 4096, 256, 232 and 291.
+static int row_limit(bool bf16, int head_dim) { return bf16 && head_dim >= 128 ? 16 : 32; }
 
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len) {
     PagedCut c;
@@ -455,7 +456,7 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
         // 36.0, 4 36.2, the rule's 35.0; one of 723 behind 20990, 56 / 8 of 64, with a cap 548, 490, 437, 420, the rule's 481; two of 2048
         // behind 6144, 32 / 8 of 128, 1 (taken) 482, 2 537; float, one of 2048 behind 20000, 8 / 2 of 128, with a cap 3417, 2636, 1993,
         // 4 (taken) 1518, 6 1567
-        const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = 256 * paged_prompt_wgs(head_dim);
+        const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = 256 * paged_prompt_wgs(bf16, head_dim);
         const double fixed = bf16 ? 1 : 18.0 / head_dim;
         const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;
         double best = 0;

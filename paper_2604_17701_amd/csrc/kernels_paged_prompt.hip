@@ -1,7 +1,7 @@
 // Attention of many rows over the paged cache: prompts, and blocks of more rows than k_paged_rows takes at once.
 //
 // A workgroup takes 128 rows of a request and KV head (its new tokens x the query heads that share the KV head), 32 per wave; keys
-// and values pass through LDS in blocks of 64 positions (float: 32), one read while the next arrives straight from the pages
+// and values pass through LDS in blocks of 64 positions (float, and head_dim 256: 32), one read while the next arrives straight from the pages
 // (global_load_lds, 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in one page).
 // On 32x32x16 products of bf16:
 //   S^T = K Q^T    the A operand's rows are dealt (bits 2 and 3 of the row swapped) so that a lane's sixteen scores of a tile are
@@ -19,14 +19,15 @@
 //
 // bf16 is bound by the matrix cores and the vector unit, which a SIMD's two or three waves, of different workgroups, overlap: the waves of one
 // workgroup run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 475 = 1.01 PFLOP/s, of
-// 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 662; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two
+// 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 510; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two
 // transcendentals a score more.  With up to 32 rows per request it is bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16
-// GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at head_dim 64, 1.4 at 128, 2.9 at 256, spread over loads, products,
+// GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at head_dim 64, 1.4 at 128, spread over loads, products,
 // exponentials and maxima.
 // Workgroups that share a CU count for more than blocks on their way: rings of 64 KB, for two workgroups, against these two blocks, for
 // three, the prompts above at head_dim 64 341 and 292, at 32 240 and 206.  At head_dim 128 three need blocks of 32 positions: 12 of 855
 // behind 187 164 and 156, but the prompts above 480 and 573, whose 1024 workgroups are no whole rounds of 768, and 64 of 32 over 8192
-// 403 and 440: two.
+// 403 and 440: two.  At head_dim 256 blocks of 32 leave registers for two instead of one: the prompts above 682 and 509, one workgroup
+// with such blocks 828.
 // Two workgroups of four waves against one of eight with the keys loaded half as often: 503 and 499 us for the prompts above, six of up
 // to 777 behind 900, 28 / 4 heads of 64, with a bias 53 and 72.  Priority to the phases of products: 481 -> 460, one of 723 behind 20990,
 // 56 / 8 of 64, with a cap 464 -> 436.  The next block's scores beside this block's exponentials in one wave, blocks of 32: 655 -> 735.
@@ -38,7 +39,7 @@ namespace wisv {
 
 typedef float paged_f16 __attribute__((ext_vector_type(16)));
 typedef __bf16 paged_bf16x2 __attribute__((ext_vector_type(2)));
-template <typename T> constexpr int BLOCK = 128 / (int)sizeof(T);   // positions: 64, float 32
+template <typename T, int HD> constexpr int BLOCK = sizeof(T) == 2 && HD < 256 ? 64 : 32;   // positions
 
 __device__ __forceinline__ paged_f16 mfma32(paged_u4 a, paged_u4 b, paged_f16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<paged_bf16x8 *>(&a), *reinterpret_cast<paged_bf16x8 *>(&b), c, 0, 0, 0);
@@ -52,14 +53,14 @@ __device__ __forceinline__ void page_to_lds(uint32_t lds_addr, uint32_t voff, co
 }
 
 constexpr int PROMPT_WAVES = 4;
-constexpr int prompt_lds(int hd) { return 4 * 128 * hd; }   // two blocks of keys and of values
+template <typename T, int HD> constexpr int prompt_lds() { return 4 * BLOCK<T, HD> * HD * (int)sizeof(T); }   // two blocks of keys and of values
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 
 template <typename T, int HD, int MODS>
-__global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(HD)) void k_paged_prompt(PagedAttn a) {
+__global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(sizeof(T) == 2, HD)) void k_paged_prompt(PagedAttn a) {
     extern __shared__ __align__(16) unsigned char lds[];   // [2][K, V][BLOCK * HD]
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int BLOCK = wisv::BLOCK<T>, RUNS = BLOCK / 16, TILES = BLOCK / 32, PER = 16 / (int)sizeof(T);   // PER: elements in 16 bytes
+    constexpr int BLOCK = wisv::BLOCK<T, HD>, RUNS = BLOCK / 16, TILES = BLOCK / 32, PER = 16 / (int)sizeof(T);   // PER: elements in 16 bytes
     constexpr int ROWS = 32 * PROMPT_WAVES, CPR = HD / PER, QT = CPR / 2, OT = HD / 32;
     constexpr float LOG2E = 1.4426950408889634f;
     constexpr int HALF = BLOCK * HD * (int)sizeof(T), BUF = 2 * HALF;   // bytes
@@ -362,9 +363,9 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(HD)) void k_pag
 int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
 template <typename T, int HD, int MODS> static const char *launch_t(PagedAttn a, int device, hipStream_t stream) {
-    a.split_steps *= 64 / BLOCK<T>;
+    a.split_steps *= 64 / BLOCK<T, HD>;
     static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
-    constexpr int lds = prompt_lds(HD);
+    constexpr int lds = prompt_lds<T, HD>();
     if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
             (void)hipGetLastError();

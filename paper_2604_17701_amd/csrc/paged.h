@@ -45,7 +45,7 @@ struct PagedCut {
 };
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len);
 // The kernel of many rows, how many of its workgroups a CU's registers and LDS have room for, and how many tiles a call has at most
-constexpr int paged_prompt_wgs(int head_dim) { return head_dim == 256 ? 1 : head_dim == 128 ? 2 : 3; }
+constexpr int paged_prompt_wgs(bool bf16, int head_dim) { return head_dim <= 64 ? 3 : bf16 || head_dim == 128 ? 2 : 1; }
 int paged_prompt_tiles(const PagedAttn &a);
 const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, int device, hipStream_t stream);
 // null, or why the launch failed
