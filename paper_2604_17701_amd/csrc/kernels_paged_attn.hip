@@ -15,7 +15,7 @@
 // Bound by bytes: 36 GB/s into one CU, about 6 TB/s into all; by latency below 100 KB per CU (a launch that reads next to nothing
 // takes 6.4 us), and float prompts by the float matrix rate.  Kernel traces: one token over 131072 positions, 32 / 8 heads of 128
 // (537 MB, 32 splits) 98 us = 5.5 TB/s; 36 tokens in windows of 4096, 16 / 8 heads of 256 (376 MB, ragged) 86 us = 4.4 TB/s; four
-// rows over 516 positions, 32 / 8 heads of 128 (2.2 MB, 4 splits) 8.7 us; 24 float requests of 40 tokens behind 4000, 32 / 8 heads of
+// rows over 516 positions, 32 / 8 heads of 128 (2.2 MB) 11.6 us; 24 float requests of 40 tokens behind 4000, 32 / 8 heads of
 // 64 (32 GFLOP), 338 us = 94 TFLOP/s of 153.  Keys and values of one step in the same registers, so that two waves share a SIMD at head_dim
 // 256, spill (99 us -> 155).
 #include "paged.h"
@@ -467,14 +467,15 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
         }
     } else {
         // One workgroup per CU.  In us: 64 keys of a head come into a CU at about 36 GB/s, a split costs 6 (its start and its
-        // end), the join and its launch 5 and the parts' way through memory.  us per call: 36 tokens in windows of 4096, 16 / 8 heads
-        // of 256, 1 split 117, 2 96, 3 96, 4 (taken) 92, 6 102; 64 blocks of 8 rows over 8192, 32 / 8 of 128, 1 376, 2 392, 4 418
+        // end), the join, its launch and its workspace 9 and the parts' way through memory.  us per call: 36 tokens in windows of 4096, 16 /
+        // 8 heads of 256, 1 split 116, 2 96, 3 96, 4 (taken) 92, 6 102; four rows over 516, 32 / 8 of 128, 1 (taken) 12.5, 2 15.7, 4
+        // 15.5, over 2004 25.7, 20.2, 16.7; 16 single tokens over 1001, 1 (taken) 18.1, 2 20.0, 4 24.6
         const int64_t wgs = (many ? std::max<int64_t>((int64_t)a.n_tokens * a.rep / (head_dim == 256 ? 16 : 32), a.batch) : a.batch) * a.G;
         const double unit = 128.0 * head_dim * (bf16 ? 2 : 4) / 36e3, part = (double)a.n_tokens * a.H * head_dim * 8 / 4e6;
         double best = 0;
         c.n_splits = 1;
         for (int s = 1; s <= PAGED_MAX_SPLITS && (s == 1 || steps / s >= 2); ++s) {
-            const double cost = (double)((wgs * s + 255) / 256) * (unit * steps / s + 6) + (s > 1 ? 5 + s * part : 0);
+            const double cost = (double)((wgs * s + 255) / 256) * (unit * steps / s + 6) + (s > 1 ? 9 + s * part : 0);
             if (s == 1 || cost < best) best = cost, c.n_splits = s;
         }
     }
