@@ -1,9 +1,9 @@
 // Attention of many rows over the paged cache: prompts, and blocks of more rows than k_paged_rows takes at once.
 //
 // A workgroup takes 128 rows of a request and KV head (its new tokens x the query heads that share the KV head), 32 per wave; keys
-// and values pass through LDS in blocks of 64 positions (float, and head_dim 256: 32), one read while the next arrives straight from the pages
-// (global_load_lds, 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in one page).
-// On 32x32x16 products of bf16:
+// and values pass through LDS in blocks of 64 positions (float, and head_dim 256: 32), one read while the next arrives straight from
+// the pages (global_load_lds, 16 bytes a lane; a wave fetches the keys and the values of the same sixteen (8) positions, which lie in
+// one page).  On 32x32x16 products of bf16:
 //   S^T = K Q^T    the A operand's rows are dealt (bits 2 and 3 of the row swapped) so that a lane's sixteen scores of a tile are
 //                  two runs of eight consecutive keys of one query ...
 //   O^T += V^T P^T ... which are, rounded to bf16, the B operand as they stand; the A operand is one 16-byte LDS read from the V
@@ -17,12 +17,13 @@
 // Float multiplies by 32x32x2 products: a lane's sixteen scores of a tile are four runs of four keys, in the order of the B operand's
 // halves, and the probabilities enter as they are.
 //
-// bf16 is bound by the matrix cores and the vector unit, which a SIMD's two or three waves, of different workgroups, overlap: the waves of one
-// workgroup run in step.  us per call among others: two prompts of 2048 behind 6144, 32 / 8 heads of 128 (481 GFLOP) 475 = 1.01 PFLOP/s, of
-// 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 510; 12 of 855 behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two
-// transcendentals a score more.  With up to 32 rows per request it is bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16
-// GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at head_dim 64, 1.4 at 128, spread over loads, products,
-// exponentials and maxima.
+// bf16 is bound by the matrix cores and the vector unit, which a SIMD's two or three waves, of different workgroups, overlap (the waves
+// of one workgroup run in step), and long calls by power: two prompts of 2048 behind 6144, 32 / 8 heads of 128, keep the matrix cores
+// busy 52 % of the cycles of a clock that falls to 1.9 GHz.  us per call among others: these (481 GFLOP) 454 to 482 = 1.0 to 1.06
+// PFLOP/s, of a library product's 1.21; the same prompts with 32 / 8 of 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 510; 12 of 855
+// behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two transcendentals a score more.  With up to 32 rows per request it is
+// bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16 GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at
+// head_dim 64, 1.4 at 128, spread over loads, products, exponentials and maxima.
 // Workgroups that share a CU count for more than blocks on their way: rings of 64 KB, for two workgroups, against these two blocks, for
 // three, the prompts above at head_dim 64 341 and 292, at 32 240 and 206.  At head_dim 128 three need blocks of 32 positions: 12 of 855
 // behind 187 164 and 156, but the prompts above 480 and 573, whose 1024 workgroups are no whole rounds of 768, and 64 of 32 over 8192
