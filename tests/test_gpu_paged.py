@@ -724,3 +724,21 @@ def test_attention_of_queries_that_are_no_numbers_over_cut_keys(ctx, dtype, new)
     assert got[1, 3].isnan().all()
     got[1, 3] = clean[1, 3]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype,dim,h,g,lens,news", [(BF16, 128, 8, 2, [200, 40], [2, 1]), (BF16, 64, 8, 2, [300, 70], [90, 64]), (BF16, 256, 4, 2, [170], [60]),
+                                                     (F32, 64, 4, 2, [200, 40], [30, 9]), (F32, 128, 32, 16, [290, 512], [256, 512])])
+@pytest.mark.parametrize("kw", [dict(scale=-0.2, softcap=7.0), dict(scale=-0.1), dict(scale=-0.3, softcap=3.0, window=40)], ids=lambda k: "-".join(k))
+def test_attention_with_a_negative_scale(ctx, dtype, dim, h, g, lens, news, kw):
+    q, kp, vp, table, starts = setup(dtype, dim, h, g, 32, lens, news, seed=11)
+    check_attention(ctx, q, kp, vp, table, starts, lens, **kw)
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF16, 32), (BF16, 64), (BF16, 128), (BF16, 256), (F32, 64), (F32, 128), (F32, 256)])
+def test_attention_of_prompts_far_into_a_cache_of_ragged_requests(ctx, dtype, dim):
+    """Idle requests, single tokens and prompts in one call, holes in the pages of some, over many blocks of keys."""
+    lens, news, h = [1500, 0, 700, 33, 900, 64], [300, 0, 1, 33, 257, 64], 32 if dtype is F32 else 4
+    q, kp, vp, table, starts = setup(dtype, dim, h, h // 2, 16, lens, news, seed=12)
+    table[0, 11] = table[4, 3] = -1
+    check_attention(ctx, q, kp, vp, table, starts, lens)
+    check_attention(ctx, q, kp, vp, table, starts, lens, window=333, prefix=[100, 0, 50, 0, 17, 64], softcap=11.0)
