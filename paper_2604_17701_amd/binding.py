@@ -387,7 +387,7 @@ class Context:
         return self.wisv_ss_decide(*args, entry="wisv_ss_decide_static", **kw)
 
     # ---------------------------------------------------------------- paged cache
-    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them.  A server makes
+    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them; no gradient flows.  A server makes
     # them once per layer and step: tensors in the usual layout are accepted by a few comparisons, the others by the helpers.
     def _stream_now(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self.device.index) or _NULL_STREAM
