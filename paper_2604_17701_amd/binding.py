@@ -387,8 +387,8 @@ class Context:
         return self.wisv_ss_decide(*args, entry="wisv_ss_decide_static", **kw)
 
     # ---------------------------------------------------------------- paged cache
-    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them; no gradient flows.  A server makes
-    # them once per layer and step: tensors in the usual layout are accepted by a few comparisons, the others by the helpers.
+    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them; no gradient flows.
+    # A server makes them once per layer and step: the checks are few comparisons per tensor, and the arguments one packed block.
     def _stream_now(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self.device.index) or _NULL_STREAM
 
