@@ -274,7 +274,9 @@ int wisv_ss_decide_static(wisv_ctx *ctx, int32_t batch, int32_t k, int32_t vocab
  *             table has a negative entry
  *   n_used    [1] entries of free_pages that were dealt
  *   status    [batch] 0, or why the request is refused (its table row stays as it was): bits 1 free_pages is exhausted,
- *             2 the table's row is too short, 4 its rows end behind max_tokens */
+ *             2 the table's row is too short, 4 its rows end behind max_tokens
+ * cached_len and new_len may lie in memory that the call writes: kv_len may be cached_len, so that a step's plan takes up the
+ * last one's (one workgroup then does the work).  Otherwise no output may overlap another, free_pages or block_table. */
 #define WISV_PAGED_NO_PAGES 1
 #define WISV_PAGED_ROW_FULL 2
 #define WISV_PAGED_NO_ROWS 4

@@ -433,7 +433,7 @@ class Context:
     def wisv_paged_plan(self, cached_len: torch.Tensor, new_len: torch.Tensor, free_pages: torch.Tensor,
                         block_table: torch.Tensor, page_size: int, max_tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
         """Plans a step: cached_len, new_len int32 [batch], free_pages int32 [n_free], block_table int32 [batch, max_pages]
-        (updated in place).  `out`: the tensors of an earlier plan of the same sizes, to be written again."""
+        (updated in place).  `out`: the tensors of an earlier plan of the same sizes, to be written again; cached_len may be its kv_len."""
         b, n_free = cached_len.numel(), free_pages.numel()
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
@@ -452,6 +452,9 @@ class Context:
             ptrs = (p, kv, pos, slots, used, used + 4)
         else:
             ptrs = [self._ints(n, t, m) for n, t, m in zip(PagePlan._fields, out, sizes)]
+            spans = sorted(zip(ptrs + [free_pages.data_ptr(), block_table.data_ptr()], sizes + (n_free, b * width)))
+            if any(p + 4 * m > q for (p, m), (q, _) in zip(spans, spans[1:])):
+                raise ValueError("the tensors of out may overlap neither each other nor free_pages and block_table")
         args = _pack_plan(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, b),
                                     self._ints("new_len", new_len, b), self._ints("free_pages", free_pages, n_free),
                                     self._ints("block_table", block_table, b, width), *ptrs, self._stream_now())

@@ -10,8 +10,8 @@ struct PagedPlan {
     const int32_t *cached_len, *new_len, *free_pages;
     int32_t *block_table, *q_start, *kv_len, *positions, *slots, *n_used, *status;
 };
-constexpr int PLAN_MAX_BATCH = 4096;   // the plan keeps two ints per request in LDS
-void launch_paged_plan(const PagedPlan &a, hipStream_t stream);
+constexpr int PLAN_MAX_BATCH = 4096;   // the plan keeps three ints per request in LDS
+void launch_paged_plan(const PagedPlan &a, bool over_lengths, hipStream_t stream);   // over_lengths: the lengths lie where it writes
 
 struct PagedAppend {
     int n_tokens, H, G, n_rope, n_pages, page_shift;

@@ -1075,6 +1075,9 @@ static int log2_of(int32_t p) {
     while (1 << s < p) ++s;
     return s;
 }
+static bool meet(const void *p, size_t p_bytes, const void *q, size_t q_bytes) {   // whether the two ranges share a byte
+    return (uintptr_t)p < (uintptr_t)q + q_bytes && (uintptr_t)q < (uintptr_t)p + p_bytes;
+}
 static bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // what the append and the attention have in common; sets the page stride when the caller left it at 0
@@ -1116,7 +1119,13 @@ extern "C" int wisv_paged_plan(wisv_ctx *ctx, const wisv_paged_plan_args *args) 
     HIP_TRY(c, dev.err);
     const PagedPlan a{p.batch, log2_of(p.page_size), p.max_pages, p.n_free, p.max_tokens, p.cached_len, p.new_len, p.free_pages,
                       p.block_table, p.q_start, p.kv_len, p.positions, p.slots, p.n_used, p.status};
-    launch_paged_plan(a, paged_stream(c, p.hip_stream));
+    // one workgroup, which reads all lengths before it writes, where an output lies over them
+    const size_t each = 4 * (size_t)p.batch, table = each * p.max_pages, rows = 4 * (size_t)p.max_tokens;
+    bool over = false;
+    for (const int32_t *len : {p.cached_len, p.new_len})
+        over |= meet(len, each, p.kv_len, each) || meet(len, each, p.q_start, each + 4) || meet(len, each, p.status, each) || meet(len, each, p.n_used, 4) ||
+                meet(len, each, p.positions, rows) || meet(len, each, p.slots, rows) || meet(len, each, p.block_table, table);
+    launch_paged_plan(a, over, paged_stream(c, p.hip_stream));
     HIP_TRY(c, hipGetLastError());
     return WISV_OK;
 }

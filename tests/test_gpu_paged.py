@@ -742,3 +742,66 @@ def test_attention_of_prompts_far_into_a_cache_of_ragged_requests(ctx, dtype, di
     table[0, 11] = table[4, 3] = -1
     check_attention(ctx, q, kp, vp, table, starts, lens)
     check_attention(ctx, q, kp, vp, table, starts, lens, window=333, prefix=[100, 0, 50, 0, 17, 64], softcap=11.0)
+
+
+# ------------------------------------------------------------------------------------------------ a plan that takes up the last one's
+
+@pytest.mark.parametrize("batch,page,hi_cached,hi_new", [(1, 16, 40, 3), (7, 16, 90, 40), (257, 64, 900, 40), (1030, 16, 70, 9), (4096, 32, 100, 5)])
+@pytest.mark.parametrize("name", ["kv_len", "q_start", "status", "positions", "slots"])
+@pytest.mark.parametrize("which", ["cached", "new"])
+def test_plan_over_its_own_lengths(ctx, batch, page, hi_cached, hi_new, name, which):
+    """An output that lies over cached_len or new_len, in step with it or an element apart: what apart gives, whoever is refused."""
+    rng = np.random.default_rng(batch)
+    cached, new = rng.integers(0, hi_cached + 1, batch), rng.integers(0, hi_new + 1, batch)
+    table, n = ref.pages_of(list(cached), page, rng)
+    wide = np.full((batch, -(-(hi_cached + hi_new) // page)), -1, np.int32)
+    wide[:, :table.shape[1]] = table
+    wide = wide[:, :max(table.shape[1], wide.shape[1] - 1)]      # the longest requests find no room in their rows
+    total = max(int(new.sum()), 1)
+    need = int(sum(-(-(c + m) // page) - -(-c // page) for c, m in zip(cached, new)))
+    for n_free, tokens in ((need, total), (need // 2, total + 50), (need, max(1, total * 2 // 3))):
+        free = n + rng.permutation(n_free)
+        want = ref.plan(cached, new, free, wide, page, tokens)
+        for apart in (0, 1):
+            sizes = dict(q_start=batch + 1, kv_len=batch, positions=tokens, slots=tokens, n_used=1, status=batch)
+            both = torch.zeros(max(sizes[name], batch) + 1, dtype=torch.int32, device=DEV)
+            lens = both[apart:apart + batch]
+            lens.copy_(ints(cached if which == "cached" else new))
+            out = binding.PagePlan(**{k: both[:m] if k == name else torch.full((m,), -77, dtype=torch.int32, device=DEV) for k, m in sizes.items()})
+            dev = ints(wide)
+            got = ctx.wisv_paged_plan(lens if which == "cached" else ints(cached), lens if which == "new" else ints(new), ints(free).reshape(-1), dev, page,
+                                      tokens, out=out)
+            for k, g, w in zip(binding.PagePlan._fields + ("block_table",), tuple(got) + (dev,), want):
+                assert g.cpu().numpy().tolist() == w.tolist(), (k, apart)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_plans_that_take_up_the_last_ones_lengths(ctx, captured):
+    """A server's steps over one set of tensors: the lengths that a plan leaves are the next one's, in place or in two sets in turn."""
+    rng = np.random.default_rng(2)
+    batch, page, tokens, width = 300, 16, 3000, 12
+    for sets in (1, 2):
+        free = ints(5 + rng.permutation(2000))
+        left, new, table = free.clone(), ints(np.zeros(batch)), ints(np.full((batch, width), -1))
+        outs = [binding.PagePlan(*[torch.zeros(n, dtype=torch.int32, device=DEV) for n in (batch + 1, batch, tokens, tokens, 1, batch)]) for _ in range(sets)]
+        steps = [lambda i=i: ctx.wisv_paged_plan(outs[i - 1].kv_len, new, left, table, page, tokens, out=outs[i]) for i in range(sets)]
+        if captured:
+            graphs = []
+            for step in steps:
+                torch.cuda.synchronize()
+                graphs.append(torch.cuda.CUDAGraph())
+                with torch.cuda.graph(graphs[-1]):
+                    step()
+            steps = [g.replay for g in graphs]
+        lens, at, host = np.zeros(batch, np.int64), 0, np.full((batch, width), -1)
+        for i in range(7):
+            ns = rng.integers(0, 9, batch) * (rng.random(batch) < 0.9)
+            new.copy_(ints(ns))
+            left.copy_(torch.cat([free[at:], free[:at]]))
+            want = ref.plan(lens, ns, left.tolist(), host, page, tokens)
+            steps[i % sets]()
+            _ = torch.randn(100, device=DEV).sum()
+            torch.cuda.synchronize()
+            for k, g, w in zip(binding.PagePlan._fields + ("block_table",), tuple(outs[i % sets]) + (table,), want):
+                assert g.cpu().numpy().tolist() == w.tolist(), (sets, i, k)
+            lens, host, at = want[1], want[6], at + int(want[4][0])

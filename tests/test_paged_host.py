@@ -278,3 +278,40 @@ def test_filling_needs_pages_for_every_position():
     assert not k.any() and not v.any()
     binding.paged_fill(k, v, [2, 0, 3], rows, rows)
     assert torch.equal(torch.cat([k[2], k[0], k[3]], 1)[:, :33], rows)
+
+
+def test_a_plan_over_its_own_lengths_is_one_workgroups(stub):
+    """Workgroups read the lengths apart from each other: where one of the outputs lies over them, a single one does the work."""
+    run(stub, '''
+        Q = lambda i: P + 4096 * i
+        apart = dict(cached_len=Q(0), new_len=Q(1), free_pages=Q(2), block_table=Q(3), q_start=Q(4), kv_len=Q(5), positions=Q(6), slots=Q(7), n_used=Q(8),
+                     status=Q(9))
+
+        def threads(**kw):
+            stub.stub_log_clear()
+            assert plan(**{**apart, **kw}) == 0 and len(log()) == 1, (text(), log())
+            return [n for n in (256, 1024) if f"ILi{n}E" in log()[0]]
+        assert threads() == [256]
+        for out in ("q_start", "kv_len", "positions", "slots", "n_used", "status", "block_table"):
+            for i in (0, 1):
+                assert threads(**{out: Q(i)}) == [1024] and threads(**{out: Q(i) + 4}) == [1024], (out, i)
+        # two requests' lengths are eight bytes: what lies beside them does not touch them
+        assert threads(kv_len=Q(0) + 8) == [256] and threads(kv_len=Q(1) - 8) == [256] and threads(kv_len=Q(1) - 4) == [1024]
+        assert threads(q_start=Q(1) - 12) == [256] and threads(q_start=Q(1) - 8) == [1024]
+    ''')
+
+
+@pytest.mark.parametrize("i", range(6))
+def test_the_binding_refuses_plans_whose_outputs_overlap(i):
+    b, tokens = 3, 10
+    lens, free, table = torch.zeros(b, dtype=torch.int32), torch.arange(12, dtype=torch.int32), torch.zeros((b, 4), dtype=torch.int32)
+    sizes = (b + 1, b, tokens, tokens, 1, b)
+    shared = torch.zeros(64, dtype=torch.int32)
+    for other in (free, table.view(-1), None):
+        out = [torch.zeros(n, dtype=torch.int32) for n in sizes]
+        if other is None:     # the last of one output is the first of the next
+            out[i], out[(i + 1) % 6] = shared[:sizes[i]], shared[sizes[i] - 1:][:sizes[(i + 1) % 6]]
+        else:
+            out[i] = other[12 - sizes[i]:]
+        with pytest.raises(ValueError, match="overlap"):
+            OnHost().wisv_paged_plan(lens, lens, free, table, 16, tokens, out=binding.PagePlan(*out))
