@@ -96,7 +96,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_paged_plan(P
     }
     // tokens: a thread each
     const int live = q_end[a.batch - 1];
-    for (int t = blockIdx.x * THREADS + tid; t < a.max_tokens; t += gridDim.x * THREADS) {
+    for (int64_t t = blockIdx.x * THREADS + tid; t < a.max_tokens; t += gridDim.x * THREADS) {   // (a step past the last may pass 32 bits)
         int pos = 0, slot = -1;
         if (t < live) {
             int lo = 0, hi = a.batch - 1;   // the first request that ends behind t

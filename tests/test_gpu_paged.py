@@ -805,3 +805,14 @@ def test_plans_that_take_up_the_last_ones_lengths(ctx, captured):
             for k, g, w in zip(binding.PagePlan._fields + ("block_table",), tuple(outs[i % sets]) + (table,), want):
                 assert g.cpu().numpy().tolist() == w.tolist(), (sets, i, k)
             lens, host, at = want[1], want[6], at + int(want[4][0])
+
+
+def test_plan_for_the_most_rows_that_a_step_can_have(ctx):
+    """2^31 - 1 rows: the count of a thread's rows ends beyond 32 bits."""
+    tokens = 2 ** 31 - 1
+    plan = ctx.wisv_paged_plan(ints([3, 70]), ints([2, 20]), ints([9, 8, 7]), ints([[4, -1], [-1] * 2]), 64, tokens)
+    assert plan.q_start.tolist() == [0, 2, 22] and plan.kv_len.tolist() == [5, 90] and plan.status.tolist() == [0, 0] and plan.n_used.tolist() == [0]
+    assert plan.positions[:22].tolist() == [3, 4] + list(range(70, 90)) and plan.slots[:3].tolist() == [259, 260, -1]
+    for rows, want in ((plan.positions, 0), (plan.slots, -1)):
+        for part in rows[22:].split(1 << 28):
+            assert int(part.min()) == want and int(part.max()) == want
