@@ -329,7 +329,7 @@ int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
  * max_new and max_len say how many new rows and how long a request is at most (0: unknown).  They choose how the work is
  * cut; requests beyond them are served all the same, more slowly.
  * Arithmetic: scores, softmax and sums in float; WISV_BF16 rounds once at the end, and probabilities enter the matrix cores as
- * one or two bf16 terms.  Equal calls give equal bits.
+ * two bf16 terms (to 2^-17) where max_new * n_heads / n_kv_heads is at most 32, else as one (to 2^-8) or two.  Equal calls give equal bits.
  * workspace: at least what wisv_paged_attention_workspace says for the same arguments (it reads no pointer but notes which are NULL);
  * nothing in it has to be cleared or kept between calls.  Calls that may overlap, and graphs that may be replayed together,
  * need one each. */

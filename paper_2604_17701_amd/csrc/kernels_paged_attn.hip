@@ -430,10 +430,10 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
 
 // Rows of a request that k_paged_rows takes: beyond them it would read the keys twice, and k_paged_prompt, which holds 128, serves
 // bf16.  From head_dim 128 on, where its two query tiles do not fit the registers, that kernel is as fast or faster from 17 rows on.  us
-// per call, k_paged_rows and k_paged_prompt: 64 requests of 32 rows, over 8192 positions, head_dim 128, two tiles of 16, 370 and 361; over
-// 4096, 256, 441 and 365; over 512, 256, 89 and 51; over 8192, 64, 187 and 213; 256 of them over 2048, 64, 221 and 204; 64 of 16 rows over
+// per call, k_paged_rows and k_paged_prompt: 64 requests of 32 rows, over 8192 positions, head_dim 128, two tiles of 16, 370 and 362; over
+// 4096, 256, 441 and 355; over 512, 256, 89 and 48; over 8192, 64, 187 and 213; 256 of them over 2048, 64, 221 and 204; 64 of 16 rows over
 // 4096, 256, 366 and 361; 37 of two rows over up to 4096, 256, 232 and 291.
-static int row_limit(bool bf16, int head_dim) { return bf16 && head_dim >= 128 ? 16 : 32; }
+static int row_limit(bool bf16, int head_dim) { return bf16 && head_dim >= 128 ? 16 : PAGED_FEW_ROWS; }
 
 PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int max_len) {
     PagedCut c;
@@ -521,7 +521,7 @@ const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max
     a.n_splits = cut.n_splits;
     if (cut.prompt) {
         a.split_steps = cut.split_steps;
-        if (const char *why = launch_paged_prompt(a, bf16, head_dim, device, stream)) return why;
+        if (const char *why = launch_paged_prompt(a, bf16, head_dim, (int64_t)a.rep * max_new <= PAGED_FEW_ROWS, device, stream)) return why;
     } else {
         a.split_steps = cut.split_steps * (bf16 ? 2 : 4);
         const int64_t rows = (int64_t)a.rep * max_new;

@@ -13,7 +13,9 @@
 // moves only when a score exceeds it by 2^8 (sums and outputs are float: nothing is lost by a reference that is too low), so that
 // rescaling the outputs is rare.
 // Probabilities enter the product as one bf16 term, an error of at most 2^-8 relative each, in the mean like that of the output's own
-// rounding: the error against 64 bits is 1.1 to 1.35 times that of a result rounded once.  Two terms cost 478 -> 600 us (below).
+// rounding: the error against 64 bits is 1.1 to 1.35 times that of a result rounded once.  Two terms cost 478 -> 600 us (below).  Where the
+// hint says that requests have at most 32 rows, one wave of a tile, memory is the bound and they are two terms p = hi + lo, |p - hi - lo| <=
+// 2^-17 p: 64 of 8 tokens over 8192, 32 / 8 heads of 128, 359 -> 363 us, with a cap 363 -> 390.  For 64 rows they would cost 361 -> 388.
 // Float multiplies by 32x32x2 products: a lane's sixteen scores of a tile are four runs of four keys, in the order of the B operand's
 // halves, and the probabilities enter as they are.
 //
@@ -22,7 +24,7 @@
 // busy 52 % of the cycles of a clock that falls to 1.9 GHz.  us per call among others: these (481 GFLOP) 454 to 482 = 1.0 to 1.06
 // PFLOP/s, of a library product's 1.21; the same prompts with 32 / 8 of 64 (241 GFLOP) 290, 16 / 8 of 256 (481 GFLOP) 510; 12 of 855
 // behind 187 with a cap, 32 / 8 of 128 (103 GFLOP) 185: a cap is two transcendentals a score more.  With up to 32 rows per request it is
-// bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16 GB) 355 = 6.1 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at
+// bound by memory: 64 of 8 tokens over 8192, 32 / 8 of 128 (2.16 GB) 363 = 5.9 TB/s.  A step of 64 keys alone on its CU takes 1.1 us at
 // head_dim 64, 1.4 at 128, spread over loads, products, exponentials and maxima.
 // Workgroups that share a CU count for more than blocks on their way: rings of 64 KB, for two workgroups, against these two blocks, for
 // three, the prompts above at head_dim 64 341 and 292, at 32 240 and 206.  At head_dim 128 three need blocks of 32 positions: 12 of 855
@@ -57,7 +59,8 @@ constexpr int PROMPT_WAVES = 4;
 template <typename T, int HD> constexpr int prompt_lds() { return 4 * BLOCK<T, HD> * HD * (int)sizeof(T); }   // two blocks of keys and of values
 enum { PLAIN = 0, CAP = 1, BIAS = 2 };   // what MODS adds to the scores
 
-template <typename T, int HD, int MODS>
+// TERMS: bf16 terms of a probability (float: one)
+template <typename T, int HD, int MODS, int TERMS>
 __global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(sizeof(T) == 2, HD)) void k_paged_prompt(PagedAttn a) {
     extern __shared__ __align__(16) unsigned char lds[];   // [2][K, V][BLOCK * HD]
     constexpr bool BF = sizeof(T) == 2;
@@ -269,16 +272,24 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(sizeof(T) == 2,
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;   // a row that has seen no key yet
         if constexpr (BF) {
-            paged_u4 p[RUNS];
+            paged_u4 p[RUNS], rest[RUNS];   // (rest: the second terms)
             const auto probs = [&](int kc) __attribute__((always_inline)) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const float x0 = x[kc >> 1][8 * (kc & 1) + 2 * w], x1 = x[kc >> 1][8 * (kc & 1) + 2 * w + 1];
                     const float e0 = __builtin_amdgcn_exp2f(MODS ? x0 - sub : fmaf(x0, scale2, -sub)), e1 = __builtin_amdgcn_exp2f(MODS ? x1 - sub : fmaf(x1, scale2, -sub));
-                    const uint32_t both = f32x2_to_bf16x2(e0, e1);
-                    p[kc][w] = both;
-                    // (the sum of what the product weighs with: rounding errors that all probabilities share cancel)
-                    l_run[w & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(paged_bf16x2, both), __builtin_bit_cast(paged_bf16x2, 0x3f803f80u), l_run[w & 1], false);
+                    if constexpr (TERMS == 2) {
+                        uint32_t hi, lo;
+                        split2x2(e0, e1, hi, lo);
+                        p[kc][w] = hi;
+                        rest[kc][w] = lo;
+                        l_run[w & 1] += e0 + e1;
+                    } else {
+                        const uint32_t both = f32x2_to_bf16x2(e0, e1);
+                        p[kc][w] = both;
+                        // (the sum of what the product weighs with: rounding errors that all probabilities share cancel)
+                        l_run[w & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(paged_bf16x2, both), __builtin_bit_cast(paged_bf16x2, 0x3f803f80u), l_run[w & 1], false);
+                    }
                 }
             };
             // a run of sixteen keys' products, and the next run's exponentials beside them
@@ -288,7 +299,11 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(sizeof(T) == 2,
 #pragma unroll
             for (int kc = 0; kc < RUNS; ++kc) {
 #pragma unroll
-                for (int dt = 0; dt < OT; ++dt) o[dt] = mfma32(*reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16), p[kc], o[dt]);
+                for (int dt = 0; dt < OT; ++dt) {
+                    const paged_u4 v = *reinterpret_cast<const paged_u4 *>(lds + vaddr + stage * BUF + (2 * kc * HD + 32 * dt) * 16);
+                    o[dt] = mfma32(v, p[kc], o[dt]);
+                    if constexpr (TERMS == 2) o[dt] = mfma32(v, rest[kc], o[dt]);
+                }
                 if (kc < RUNS - 1) probs(kc + 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -363,38 +378,38 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, paged_prompt_wgs(sizeof(T) == 2,
 
 int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * a.rep / (32 * PROMPT_WAVES)) + a.batch; }
 
-template <typename T, int HD, int MODS> static const char *launch_t(PagedAttn a, int device, hipStream_t stream) {
+template <typename T, int HD, int MODS, int TERMS> static const char *launch_t(PagedAttn a, int device, hipStream_t stream) {
     a.split_steps *= 64 / BLOCK<T, HD>;
     static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
     constexpr int lds = prompt_lds<T, HD>();
     if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS, TERMS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
             (void)hipGetLastError();
             return "the device refuses the kernel's LDS request";
         }
         if (device >= 0 && device < MAX_DEVICES) allowed[device] = true;
     }
-    hipLaunchKernelGGL((k_paged_prompt<T, HD, MODS>), dim3(paged_prompt_tiles(a) * a.G, a.n_splits), dim3(64 * PROMPT_WAVES), lds, stream, a);
+    hipLaunchKernelGGL((k_paged_prompt<T, HD, MODS, TERMS>), dim3(paged_prompt_tiles(a) * a.G, a.n_splits), dim3(64 * PROMPT_WAVES), lds, stream, a);
     return nullptr;
 }
-template <typename T, int HD> static const char *launch_m(const PagedAttn &a, int device, hipStream_t stream) {
+template <typename T, int HD, int TERMS> static const char *launch_m(const PagedAttn &a, int device, hipStream_t stream) {
     const bool cap = a.softcap > 0.f;
     // (PLAIN scales the maximum in the place of the scores, which only a positive scale keeps a maximum)
-    if (a.slopes || (a.scale < 0.f && !cap)) return cap ? launch_t<T, HD, CAP | BIAS>(a, device, stream) : launch_t<T, HD, BIAS>(a, device, stream);
-    return cap ? launch_t<T, HD, CAP>(a, device, stream) : launch_t<T, HD, PLAIN>(a, device, stream);
+    if (a.slopes || (a.scale < 0.f && !cap)) return cap ? launch_t<T, HD, CAP | BIAS, TERMS>(a, device, stream) : launch_t<T, HD, BIAS, TERMS>(a, device, stream);
+    return cap ? launch_t<T, HD, CAP, TERMS>(a, device, stream) : launch_t<T, HD, PLAIN, TERMS>(a, device, stream);
 }
-template <typename T> static const char *launch_d(const PagedAttn &a, int head_dim, int device, hipStream_t stream) {
+template <int HD> static const char *launch_bf16(const PagedAttn &a, bool few, int device, hipStream_t stream) {
+    if constexpr (HD >= 128)   // (smaller heads: few rows are k_paged_rows's, by paged_cut)
+        if (few) return launch_m<bf16_t, HD, 2>(a, device, stream);
+    return launch_m<bf16_t, HD, 1>(a, device, stream);
+}
+const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, bool few, int device, hipStream_t stream) {
     switch (head_dim) {
-        case 32:
-            if constexpr (sizeof(T) == 2) return launch_m<T, 32>(a, device, stream);   // (float, head_dim 32: k_paged_rows, by paged_cut)
-            return "no such kernel";
-        case 64: return launch_m<T, 64>(a, device, stream);
-        case 128: return launch_m<T, 128>(a, device, stream);
-        default: return launch_m<T, 256>(a, device, stream);
+        case 32: return bf16 ? launch_bf16<32>(a, few, device, stream) : "no such kernel";   // (float, head_dim 32: k_paged_rows, by paged_cut)
+        case 64: return bf16 ? launch_bf16<64>(a, few, device, stream) : launch_m<float, 64, 1>(a, device, stream);
+        case 128: return bf16 ? launch_bf16<128>(a, few, device, stream) : launch_m<float, 128, 1>(a, device, stream);
+        default: return bf16 ? launch_bf16<256>(a, few, device, stream) : launch_m<float, 256, 1>(a, device, stream);
     }
-}
-const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, int device, hipStream_t stream) {
-    return bf16 ? launch_d<bf16_t>(a, head_dim, device, stream) : launch_d<float>(a, head_dim, device, stream);
 }
 
 }  // namespace wisv

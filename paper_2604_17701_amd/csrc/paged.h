@@ -47,7 +47,9 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
 // The kernel of many rows, how many of its workgroups a CU's registers and LDS have room for, and how many tiles a call has at most
 constexpr int paged_prompt_wgs(bool bf16, int head_dim) { return head_dim <= 64 ? 3 : bf16 || head_dim == 128 ? 2 : 1; }
 int paged_prompt_tiles(const PagedAttn &a);
-const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, int device, hipStream_t stream);
+// few: requests have at most PAGED_FEW_ROWS rows, by the hint
+constexpr int PAGED_FEW_ROWS = 32;
+const char *launch_paged_prompt(const PagedAttn &a, bool bf16, int head_dim, bool few, int device, hipStream_t stream);
 // null, or why the launch failed
 const char *launch_paged_attention(PagedAttn a, bool bf16, int head_dim, int max_new, int max_len, int device, hipStream_t stream);
 

@@ -14,6 +14,7 @@ import torch
 
 from oracle import paged as ref
 from paper_2604_17701_amd import binding
+from parity import record
 from wisv_inputs import configs, gen
 
 pytestmark = pytest.mark.gpu
@@ -816,3 +817,43 @@ def test_plan_for_the_most_rows_that_a_step_can_have(ctx):
     for rows, want in ((plan.positions, 0), (plan.slots, -1)):
         for part in rows[22:].split(1 << 28):
             assert int(part.min()) == want and int(part.max()) == want
+
+
+# ------------------------------------------------------------------------------------------------ the terms of a probability
+
+@pytest.mark.parametrize("dim,h,g,news", [(32, 8, 2, [8, 3, 1]), (64, 8, 2, [4, 4, 1]), (64, 12, 3, [8, 8, 5]), (128, 8, 2, [4, 1, 3]), (128, 8, 2, [8, 5, 8]),
+                                          (128, 3, 1, [6, 10, 9]), (256, 4, 1, [4, 4, 1]), (256, 8, 2, [8, 1, 7])])
+@pytest.mark.parametrize("window", [0, 90])
+def test_few_rows_have_probabilities_of_two_terms(ctx, dim, h, g, news, window):
+    """Up to 32 rows per KV head, by the hint: probabilities are good to 2^-17, which one bf16 term is not.
+
+    Queries and keys are small integers, so that products and their sums are exact and a score x (in units of ln 2) is off by the
+    rounding of the scale, of its product and of the difference to the maximum, 2^-24 * 2 max|x| each.  An exponential adds 2^-23, each
+    of at most four moves of the maximum 2^-23 and a rounding, twice (sum and output): delta = (6 max|x| + 20) * 2^-24.  The rest as above,
+    with 2^-17 for a probability.  Outputs near zero show it: what is rounded at the end is small there."""
+    lens = [160, 97, 130]
+    rng = np.random.default_rng(dim + h)
+    table, n_pages = ref.pages_of(lens, 16, rng)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    whole = lambda *shape: torch.from_numpy(rng.integers(-2, 3, shape).astype(np.float32)).to(BF16).to(DEV)  # noqa: E731
+    q, kp, scale = whole(int(starts[-1]), h, dim), whole(n_pages, g, 16, dim), 2.0 ** -5
+    vp = normal(dim, (n_pages, g, 2, dim, 8), BF16)
+    got = f64(ctx.wisv_paged_attention(q, kp, vp, ints(table), ints(starts), ints(lens), max(news), max(lens), scale=scale, window=window))
+    qh, kh, vh = f64(q), f64(kp), f64(vp)
+    out, mass, _ = ref.attention(qh, kh, vh, table, starts, lens, scale=scale, window=window)
+    one, x_max = np.zeros_like(out), 0.0
+    for b, n in enumerate(news):     # what one term would give
+        k, v, _ = ref.gather(kh, vh, table[b], lens[b])
+        p, j = (lens[b] - n + np.arange(n))[:, None], np.arange(lens[b])[None, :]
+        sees = (j <= p) & (j > p - (window or 10 ** 6))
+        for head in range(h):
+            x = np.where(sees, scale * (qh[starts[b]:starts[b + 1], head] @ k[head // (h // g)].T), -np.inf)
+            x_max = max(x_max, np.abs(x[sees]).max() / np.log(2.0))
+            e = f64(torch.from_numpy(np.exp(x - x.max(1, keepdims=True))).to(BF16))
+            one[starts[b]:starts[b + 1], head] = e @ v[head // (h // g)] / e.sum(1, keepdims=True)
+    delta = (6 * x_max + 20) * 2.0 ** -24
+    lim = 2.0 ** -8 * np.abs(out) + (2.0 ** -17 + 2 * delta + (max(lens) + 64) * 2.0 ** -24) * mass
+    assert (np.abs(one - out) > lim).mean() > 0.01
+    err = np.abs(got - out)
+    record(f"paged_two_terms_{dim}_{h}_{g}_{max(news)}_w{window}", {"err_of_limit": float((err / lim).max()), "one_term_of_limit": float((np.abs(one - out) / lim).max())})
+    assert (err <= lim).all(), (err / lim).max()
