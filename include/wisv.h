@@ -298,7 +298,7 @@ int wisv_paged_plan(wisv_ctx *ctx, const wisv_paged_plan_args *args);
  * c = cos[position][i], s = sin[position][i], the pair (x_i, x_{i + half}) becomes (x_i c - x_{i + half} s,
  * x_{i + half} c + x_i s), in float, rounded once.  Rows whose slot lies outside the pool store no key and no value (their
  * queries are rotated all the same); of two rows with one slot either may leave an element there.  Positions outside the tables take the nearest
- * row of them.  q_out may be q (with the same stride). */
+ * row of them.  q_out may be q (with the same stride); otherwise what the call writes overlaps nothing that it reads. */
 typedef struct {
     int32_t n_tokens;            /* 0: nothing to do */
     int32_t n_heads, n_kv_heads; /* n_heads 0: there are no queries (q, q_out NULL) */
@@ -326,6 +326,7 @@ int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
  * Keys and values that a row does not see do not reach its output, whatever they hold; a value that it sees and that is
  * not finite makes that feature of its output infinite or NaN.  Rows of q behind q_start[batch] are
  * neither read nor written, nor are those before q_start[0].  kv_len beyond max_pages * page_size leaves the positions behind the table unseen.
+ * out may be q (with the same stride); otherwise what the call writes, the workspace included, overlaps nothing that it reads.
  * max_new and max_len say how many new rows and how long a request is at most (0: unknown).  They choose how the work is
  * cut; requests beyond them are served all the same, more slowly.
  * Arithmetic: scores, softmax and sums in float; WISV_BF16 rounds once at the end, and probabilities enter the matrix cores as

@@ -117,6 +117,15 @@ def _packer(args):
 _pack_plan, _pack_append, _pack_attention = (_packer(t) for t in (wisv_paged_plan_args, wisv_paged_append_args, wisv_paged_attention_args))
 
 
+def _rows_meet(p: int, p_stride: int, p_width: int, q: int, q_stride: int, q_width: int, rows: int) -> bool:
+    """Whether `rows` rows of p_width bytes, p_stride apart, share a byte with rows of q_width, q_stride apart (columns of one packed
+    row do not; other rows that lie among each other are taken to)."""
+    if p + (rows - 1) * p_stride + p_width <= q or q + (rows - 1) * q_stride + q_width <= p or rows < 1:
+        return False
+    off = (q - p) % p_stride if p_stride else 0
+    return p_stride != q_stride or off < p_width or off + q_width > p_stride
+
+
 class PagePlan(NamedTuple):
     """What wisv_paged_plan leaves (int32 device tensors; wisv.h says what they hold)."""
     q_start: torch.Tensor
@@ -412,6 +421,25 @@ class Context:
             raise ValueError(f"the heads of a row of {name} must lie close together")
         return t.data_ptr(), heads, s0 if rows > 1 else heads * head_dim
 
+    def _result(self, name: str, t: torch.Tensor, dtype, rows: int, head_dim: int, heads: int, inputs, pools, pool_size: int):
+        """(pointer, row stride) of the rows that a call writes.  They may be its first input's, element by element (inputs: pointer, row
+        stride and heads of each); otherwise they lie apart from the inputs and the pools (pointers, and elements of either)."""
+        p, h, s = self._rows(name, t, dtype, rows, head_dim)
+        if h != heads:
+            raise ValueError(f"{name} must have the heads of q")
+        e = 2 if dtype is torch.bfloat16 else 4
+        w = heads * head_dim
+        end = p + ((rows - 1) * s + w) * e
+        bad = False
+        for i, (q, qs, qh) in enumerate(inputs):     # (what lies wholly apart is not looked at closer)
+            if q < end and p < q + ((rows - 1) * qs + qh * head_dim) * e and (i or q != p or qs != s):
+                bad |= _rows_meet(p, s * e, w * e, q, qs * e, qh * head_dim * e, rows)
+        for x in pools:
+            bad |= x < end and p < x + pool_size * e and rows > 0
+        if bad:
+            raise ValueError(f"{name} may be q with the same strides, and else must overlap neither the other tensors nor the pools")
+        return p, s
+
     def _pools(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         """(pages, KV heads, page size, head_dim, wisv_dtype, page stride) of a pair of pools."""
         dt, dev, shape = k_pages.dtype, self.device.index, k_pages.shape
@@ -452,9 +480,13 @@ class Context:
             ptrs = (p, kv, pos, slots, used, used + 4)
         else:
             ptrs = [self._ints(n, t, m) for n, t, m in zip(PagePlan._fields, out, sizes)]
-            spans = sorted(zip(ptrs + [free_pages.data_ptr(), block_table.data_ptr()], sizes + (n_free, b * width)))
-            if any(p + 4 * m > q for (p, m), (q, _) in zip(spans, spans[1:])):
-                raise ValueError("the tensors of out may overlap neither each other nor free_pages and block_table")
+            p, kv, pos, slots, used, st = ptrs
+            f, t, end = free_pages.data_ptr(), block_table.data_ptr(), st + 4 * b
+            if not (p + 4 * b < kv and kv + 4 * b <= pos and pos + 4 * max_tokens <= slots and slots + 4 * max_tokens <= used < st
+                    and (f + 4 * n_free <= p or end <= f) and (t + 4 * b * width <= p or end <= t)):     # (not a plan of this function's own)
+                spans = sorted(zip(ptrs + [f, t], sizes + (n_free, b * width)))
+                if any(p + 4 * m > q for (p, m), (q, _) in zip(spans, spans[1:])):
+                    raise ValueError("the tensors of out may overlap neither each other nor free_pages and block_table")
         args = _pack_plan(b, page_size, width, n_free, max_tokens, self._ints("cached_len", cached_len, b),
                                     self._ints("new_len", new_len, b), self._ints("free_pages", free_pages, n_free),
                                     self._ints("block_table", block_table, b, width), *ptrs, self._stream_now())
@@ -468,7 +500,7 @@ class Context:
                           sin: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Rotates the rows' queries and keys (float32 tables cos, sin [n_rope, head_dim / 2]; None: they stay as they are) and
         stores keys and values into their slots.  q [tokens, heads, head_dim] or None, k, v [tokens, kv heads, head_dim], slices
-        of a packed row included; positions, slots int32 [tokens].  Returns the rotated queries (q_out, which may be q)."""
+        of a packed row included; positions, slots int32 [tokens].  Returns the rotated queries (q_out, which may be q with its strides)."""
         n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)
         rows, dt = k.shape[0], k_pages.dtype
         kp, kg, ks = self._rows("k", k, dt, rows, hd)
@@ -482,9 +514,8 @@ class Context:
                 q_out = torch.empty_like(q)   # (contiguous: the heads of a row of q lie close together)
                 qop, qos = q_out.data_ptr(), heads * hd
             else:
-                qop, oh, qos = self._rows("q_out", q_out, dt, rows, hd)
-                if oh != heads:
-                    raise ValueError("q_out must have the heads of q")
+                qop, qos = self._result("q_out", q_out, dt, rows, hd, heads, ((qp, qs, heads), (kp, ks, g), (vp, vs, g)),
+                                        (k_pages.data_ptr(), v_pages.data_ptr()), (n - 1) * stride + g * ps * hd)
         elif q_out is not None:
             raise ValueError("q_out without q")
         if positions is not None:
@@ -509,8 +540,8 @@ class Context:
                              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the rows q [tokens, heads, head_dim] over the pages; q_start int32 [batch + 1], kv_len int32 [batch],
         block_table int32 [batch, max_pages], slopes float32 [heads], prefix_len int32 [batch].  max_new, max_len: how many
-        new rows and how many positions a request has at most (0: unknown).  A new `out` is made where none is given: rows
-        behind q_start[batch] are left as they are in either.  workspace: a tensor of at least as many bytes as
+        new rows and how many positions a request has at most (0: unknown).  A new `out` is made where none is given (it may be q with
+        its strides): rows behind q_start[batch] are left as they are in either.  workspace: a tensor of at least as many bytes as
         wisv_paged_attention_workspace asks for, kept by a caller whose calls must not allocate."""
         n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)
         rows, dt = q.shape[0], k_pages.dtype
@@ -519,9 +550,7 @@ class Context:
             out = torch.empty_like(q)   # (contiguous: the heads of a row of q lie close together)
             op, os_ = out.data_ptr(), heads * hd
         else:
-            op, oh, os_ = self._rows("out", out, dt, rows, hd)
-            if oh != heads:
-                raise ValueError("out must have the heads of q")
+            op, os_ = self._result("out", out, dt, rows, hd, heads, ((qp, qs, heads),), (k_pages.data_ptr(), v_pages.data_ptr()), (n - 1) * stride + g * ps * hd)
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
         if not (abs(max_new) < 1 << 31 and abs(max_len) < 1 << 31 and abs(window) < 1 << 31):

@@ -857,3 +857,17 @@ def test_few_rows_have_probabilities_of_two_terms(ctx, dim, h, g, news, window):
     err = np.abs(got - out)
     record(f"paged_two_terms_{dim}_{h}_{g}_{max(news)}_w{window}", {"err_of_limit": float((err / lim).max()), "one_term_of_limit": float((np.abs(one - out) / lim).max())})
     assert (err <= lim).all(), (err / lim).max()
+
+
+@pytest.mark.parametrize("dtype,dim,lens,news", [(BF16, 128, [300, 70], [3, 1]), (BF16, 128, [300, 70], [90, 64]), (BF16, 64, [5000], [2]), (BF16, 64, [9000], [60]),
+                                                 (F32, 64, [300, 70], [40, 9]), (F32, 64, [5000], [4])])
+def test_attention_in_place(ctx, dtype, dim, lens, news):
+    """out over q itself, in packed rows: what another tensor gets, and nothing beside the queries is touched."""
+    h, g = 8, 2
+    q, kp, vp, table, starts = setup(dtype, dim, h, g, 16, lens, news)
+    args = (kp, vp, ints(table), ints(starts), ints(lens), max(news), max(lens))
+    want = ctx.wisv_paged_attention(q, *args)
+    packed = torch.full((q.shape[0], h + 3, dim), 7.0, dtype=dtype, device=DEV)
+    packed[:, 1:1 + h] = q
+    got = ctx.wisv_paged_attention(packed[:, 1:1 + h], *args, out=packed[:, 1:1 + h])
+    assert torch.equal(got, want) and (packed[:, 0] == 7).all() and (packed[:, 1 + h:] == 7).all()

@@ -315,3 +315,42 @@ def test_the_binding_refuses_plans_whose_outputs_overlap(i):
             out[i] = other[12 - sizes[i]:]
         with pytest.raises(ValueError, match="overlap"):
             OnHost().wisv_paged_plan(lens, lens, free, table, 16, tokens, out=binding.PagePlan(*out))
+
+
+def test_which_rows_meet():
+    """Against the bytes themselves."""
+    import itertools
+    for p, s, w, q, t, v, n in itertools.product((0, 3, 8), (4, 8, 9), (1, 4), (0, 1, 5, 12, 30), (4, 8), (2, 4), (1, 2, 3)):
+        a, b = ({x + i * y + j for i in range(n) for j in range(z)} for x, y, z in ((p, s, w), (q, t, v)))
+        got = binding._rows_meet(p, s, w, q, t, v, n)
+        assert got or not a & b
+        assert not got or a & b or s != t, (p, s, w, q, t, v, n)
+
+
+def test_the_binding_refuses_results_over_what_a_call_reads():
+    h, g, hd, n = 4, 2, 32, 6
+    buf = torch.zeros((40, h + 2 * g + 2, hd))
+    q, k, v = buf[4:4 + n, :h], buf[4:4 + n, h:h + g], buf[4:4 + n, h + g:h + 2 * g]
+    pools = torch.zeros((2, 3, g, 16, hd))
+    kp, vp = pools[0], pools[1].view(3, g, 2, hd, 8)
+    ints = torch.zeros(n, dtype=torch.int32)
+    lens, starts, table = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros((1, 2), dtype=torch.int32)
+    one = buf.view(-1)
+    over = {"a head further": buf[4:4 + n, 1:1 + h], "a row further": buf[5:5 + n, :h], "from the keys on": buf[4:4 + n, h - 1:2 * h - 1], "another stride":
+            one[4 * buf.stride(0):].as_strided((n, h, hd), (h * hd, hd, 1)), "the keys' pool": pools.view(-1)[64:].as_strided((n, h, hd), (h * hd, hd, 1)),
+            "the values' pool": pools.view(-1)[pools[0].numel() + 512:].as_strided((n, h, hd), (h * hd, hd, 1))}
+    for what, out in over.items():
+        with pytest.raises(ValueError, match="overlap"):
+            OnHost().wisv_paged_append(q, k, v, None, ints, kp, vp, q_out=out)
+        if what != "from the keys on":
+            with pytest.raises(ValueError, match="overlap"):
+                OnHost().wisv_paged_attention(q, kp, vp, table, starts, lens, out=out)
+    with pytest.raises(ValueError, match="overlap"):
+        OnHost().wisv_paged_append(q, buf[4:4 + n, h - 1:h + 1], v, None, ints, kp, vp, q_out=q)     # in place, over a head of the keys
+    with pytest.raises(ValueError, match="overlap"):
+        OnHost().wisv_paged_append(k, k, v, None, ints, kp, vp, q_out=k)
+    with pytest.raises(ValueError, match="heads of q"):
+        OnHost().wisv_paged_attention(q, kp, vp, table, starts, lens, out=torch.zeros((n, h + 1, hd)))
+    result = lambda out: OnHost()._result("out", out, torch.float32, n, hd, h, ((q.data_ptr(), q.stride(0), h), (k.data_ptr(), k.stride(0), g)), (kp.data_ptr(), vp.data_ptr()), kp.numel())  # noqa: E731
+    for out in (q, torch.zeros((n, h, hd)), buf[10:10 + n, :h], buf[4:4 + n, h + g:]):     # in place, elsewhere, rows behind, columns beside
+        assert result(out) == (out.data_ptr(), out.stride(0))
