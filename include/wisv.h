@@ -341,7 +341,7 @@ typedef struct {
     int32_t max_pages; /* max_pages * page_size at most 2^30 */
     int32_t max_new, max_len;
     int32_t window;   /* 0: none */
-    float scale;      /* 0: 1 / sqrt(head_dim) */
+    float scale;      /* 0: 1 / sqrt(head_dim); else at most 1e38 in magnitude, and so is scale / softcap */
     float softcap;    /* 0: none; else from 1e-30 to 16384 */
     const void *q;
     void *out;

@@ -1180,6 +1180,10 @@ static int paged_attention_args(Ctx *c, const wisv_paged_attention_args *args, P
     // (bf16 calls have a cap's tanh to 2^-23 of the cap: up to 2^14 that is within a probability's own rounding)
     if ((p.softcap != 0.f && !(p.softcap >= 1e-30f && p.softcap <= 16384.f)) || !isfinite(p.scale))
         return fail(c, WISV_EINVAL, "wisv_paged_attention: softcap must be 0 or from 1e-30 to 16384, scale finite");
+    // (the kernels hold 2 scale / ln 2, divided by a cap: infinite, it would make a score of 0 no number)
+    const float steep = 2.885390082f * (p.scale != 0.f ? p.scale : 1.f);
+    if (!isfinite(steep) || (p.softcap != 0.f && !isfinite(steep / p.softcap)))
+        return fail(c, WISV_EINVAL, "wisv_paged_attention: scale, or scale / softcap, is too large: it must be at most 1e38");
     const int64_t width = (int64_t)p.n_heads * p.head_dim;
     if (p.batch && p.n_tokens) {
         if (!rows_ok(p.q, p.q_stride, width, p.dtype) || !rows_ok(p.out, p.out_stride, width, p.dtype))

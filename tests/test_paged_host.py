@@ -354,3 +354,17 @@ def test_the_binding_refuses_results_over_what_a_call_reads():
     result = lambda out: OnHost()._result("out", out, torch.float32, n, hd, h, ((q.data_ptr(), q.stride(0), h), (k.data_ptr(), k.stride(0), g)), (kp.data_ptr(), vp.data_ptr()), kp.numel())  # noqa: E731
     for out in (q, torch.zeros((n, h, hd)), buf[10:10 + n, :h], buf[4:4 + n, h + g:]):     # in place, elsewhere, rows behind, columns beside
         assert result(out) == (out.data_ptr(), out.stride(0))
+
+
+def test_settings_beyond_the_arithmetic_are_refused(stub):
+    """2 scale / (ln 2 softcap) beyond float would make the score of orthogonal vectors, 0, no number."""
+    run(stub, '''
+        for kw in (dict(scale=3e38), dict(scale=-2e38), dict(scale=1e9, softcap=1e-30), dict(scale=-1e9, softcap=1e-30), dict(scale=1e38, softcap=0.5)):
+            assert np.isinf(np.float32(2.885390082) * np.float32(kw["scale"])) or np.isinf(np.float32(2.885390082) * np.float32(kw["scale"]) / np.float32(kw["softcap"]))
+            assert attn(**kw) == B.WISV_EINVAL and "scale" in text(), kw
+            n = C.c_size_t()
+            assert lib.wisv_paged_attention_workspace(h, C.byref(attn_args(**kw)), C.byref(n)) == B.WISV_EINVAL
+        assert log() == []
+        for kw in (dict(scale=1e38), dict(scale=-1e38), dict(scale=1e8, softcap=1e-30), dict(scale=1e38, softcap=16384.0), dict(softcap=1e-30)):
+            assert attn(**kw) == 0, (kw, text())
+    ''')
