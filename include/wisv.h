@@ -262,7 +262,7 @@ int wisv_ss_decide_static(wisv_ctx *ctx, int32_t batch, int32_t k, int32_t vocab
  *   head_dim    32, 64, 128 or 256; dtype wisv_dtype of q, k, v, both pools and the output.  Pointers lie on 16 bytes,
  *               strides are multiples of 16 bytes; the heads of a row lie close together.
  *   hip_stream  the stream the call enqueues on: NULL is the ctx's, hipStreamLegacy the null stream.
- * Calls that share no output or workspace may overlap on different streams.
+ * Calls that share no output or workspace may overlap on different streams.  They serve: no gradient is computed.
  */
 
 /* A step's plan from the lengths of its requests.  Request b holds cached_len[b] tokens and brings new_len[b] (negative

@@ -117,6 +117,11 @@ def _packer(args):
 _pack_plan, _pack_append, _pack_attention = (_packer(t) for t in (wisv_paged_plan_args, wisv_paged_append_args, wisv_paged_attention_args))
 
 
+def _no_gradient(name: str):
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and none flows through this call: detach it or call under torch.no_grad()")
+
+
 def _rows_meet(p: int, p_stride: int, p_width: int, q: int, q_stride: int, q_width: int, rows: int) -> bool:
     """Whether `rows` rows of p_width bytes, p_stride apart, share a byte with rows of q_width, q_stride apart (columns of one packed
     row do not; other rows that lie among each other are taken to)."""
@@ -396,7 +401,8 @@ class Context:
         return self.wisv_ss_decide(*args, entry="wisv_ss_decide_static", **kw)
 
     # ---------------------------------------------------------------- paged cache
-    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them; no gradient flows.
+    # These take device tensors and enqueue on torch's current stream of the ctx's device; wisv.h describes them.  No gradient flows: under
+    # autograd, rows and slopes that want one are refused.
     # A server makes them once per layer and step: the checks are few comparisons per tensor, and the arguments one packed block.
     def _stream_now(self) -> int:
         return torch._C._cuda_getCurrentRawStream(self.device.index) or _NULL_STREAM
@@ -419,6 +425,8 @@ class Context:
         heads, (s0, s1, s2) = shape[1], t.stride()
         if (s2 != 1 or (s1 != head_dim and heads > 1)) and t.numel():
             raise ValueError(f"the heads of a row of {name} must lie close together")
+        if t.requires_grad:
+            _no_gradient(name)
         return t.data_ptr(), heads, s0 if rows > 1 else heads * head_dim
 
     def _result(self, name: str, t: torch.Tensor, dtype, rows: int, head_dim: int, heads: int, inputs, pools, pool_size: int):
@@ -500,7 +508,8 @@ class Context:
                           sin: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Rotates the rows' queries and keys (float32 tables cos, sin [n_rope, head_dim / 2]; None: they stay as they are) and
         stores keys and values into their slots.  q [tokens, heads, head_dim] or None, k, v [tokens, kv heads, head_dim], slices
-        of a packed row included; positions, slots int32 [tokens].  Returns the rotated queries (q_out, which may be q with its strides)."""
+        of a packed row included; positions, slots int32 [tokens].  Returns the rotated queries (q_out, which may be q with its strides),
+        without a gradient."""
         n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)
         rows, dt = k.shape[0], k_pages.dtype
         kp, kg, ks = self._rows("k", k, dt, rows, hd)
@@ -538,7 +547,7 @@ class Context:
                              softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None,
                              prefix_len: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention of the rows q [tokens, heads, head_dim] over the pages; q_start int32 [batch + 1], kv_len int32 [batch],
+        """Attention of the rows q [tokens, heads, head_dim] over the pages, without a gradient; q_start int32 [batch + 1], kv_len int32 [batch],
         block_table int32 [batch, max_pages], slopes float32 [heads], prefix_len int32 [batch].  max_new, max_len: how many
         new rows and how many positions a request has at most (0: unknown).  A new `out` is made where none is given (it may be q with
         its strides): rows behind q_start[batch] are left as they are in either.  workspace: a tensor of at least as many bytes as
@@ -550,13 +559,16 @@ class Context:
             out = torch.empty_like(q)   # (contiguous: the heads of a row of q lie close together)
             op, os_ = out.data_ptr(), heads * hd
         else:
-            op, os_ = self._result("out", out, dt, rows, hd, heads, ((qp, qs, heads),), (k_pages.data_ptr(), v_pages.data_ptr()), (n - 1) * stride + g * ps * hd)
+            op, os_ = self._result("out", out, dt, rows, hd, heads, ((qp, qs, heads),), (k_pages.data_ptr(), v_pages.data_ptr()),
+                                   (n - 1) * stride + g * ps * hd)
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
         if not (abs(max_new) < 1 << 31 and abs(max_len) < 1 << 31 and abs(window) < 1 << 31):
             raise ValueError("max_new, max_len and window must fit 32 bits")
         if 0 < abs(scale) < 1e-37 or 0 < softcap < 1e-37 or abs(scale) > 1e38 or softcap > 1e38:   # (0 means something else)
             raise ValueError("scale and softcap must be float32 numbers")
+        if slopes is not None and slopes.requires_grad:
+            _no_gradient("slopes")
         b, width = kv_len.numel(), block_table.shape[1]
         args = (b, rows, heads, g, hd, dtype, ps, n, width, max_new, max_len, window, scale, softcap, qp, op, qs, os_,
                 k_pages.data_ptr(), v_pages.data_ptr(), stride, self._ints("block_table", block_table, b, width),

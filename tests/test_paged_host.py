@@ -368,3 +368,20 @@ def test_settings_beyond_the_arithmetic_are_refused(stub):
         for kw in (dict(scale=1e38), dict(scale=-1e38), dict(scale=1e8, softcap=1e-30), dict(scale=1e38, softcap=16384.0), dict(softcap=1e-30)):
             assert attn(**kw) == 0, (kw, text())
     ''')
+
+
+def test_the_binding_refuses_rows_that_want_a_gradient():
+    h, g, hd, n = 4, 2, 32, 6
+    q, k, v = torch.zeros(n, h, hd), torch.zeros(n, g, hd), torch.zeros(n, g, hd)
+    kp, vp = binding.new_paged_cache(3, g, 16, hd, torch.float32, "cpu")
+    ints, lens, starts, table = (torch.zeros(m, dtype=torch.int32) for m in (n, 1, 2, 2))
+    args = dict(block_table=table.view(1, 2), q_start=starts, kv_len=lens)
+    want = lambda t: (t * 1.0).requires_grad_()  # noqa: E731
+    for rows in ((want(q), k, v), (q, want(k), v), (q, k, want(v))):
+        with pytest.raises(ValueError, match="gradient"):
+            OnHost().wisv_paged_append(*rows, None, ints, kp, vp)
+    for kw in (dict(q=want(q)), dict(q=q, out=want(q)), dict(q=want(q) * 2), dict(q=q, slopes=want(torch.zeros(h)))):
+        with pytest.raises(ValueError, match="gradient"):
+            OnHost().wisv_paged_attention(**{**dict(k_pages=kp, v_pages=vp, **args), **kw})
+    for call in (lambda: OnHost()._rows("q", want(q).detach(), torch.float32, n, hd), torch.no_grad()(lambda: OnHost()._rows("q", want(q), torch.float32, n, hd))):
+        assert call()[1:] == (h, h * hd)
