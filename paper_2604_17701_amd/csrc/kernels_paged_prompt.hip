@@ -36,6 +36,8 @@
 // 56 / 8 of 64, with a cap 464 -> 436.  The next block's scores beside this block's exponentials in one wave, blocks of 32: 655 -> 735.
 // Float is bound by the matrix cores, whose 64 cycles a product hide the rest: one prompt of 2048 behind 20000, 8 / 2 heads of 128 (176
 // GFLOP) 1357 us = 130 TFLOP/s (k_paged_rows 1707; a library's product of 8192^3 153).
+#include <atomic>
+
 #include "paged.h"
 
 namespace wisv {
@@ -380,7 +382,7 @@ int paged_prompt_tiles(const PagedAttn &a) { return (int)((int64_t)a.n_tokens * 
 
 template <typename T, int HD, int MODS, int TERMS> static const char *launch_t(PagedAttn a, int device, hipStream_t stream) {
     a.split_steps *= 64 / BLOCK<T, HD>;
-    static bool allowed[MAX_DEVICES];   // a cache of an idempotent call, not state that results depend on
+    static std::atomic<bool> allowed[MAX_DEVICES];   // a cache of an idempotent call (of any thread), not state that results depend on
     constexpr int lds = prompt_lds<T, HD>();
     if (!(device >= 0 && device < MAX_DEVICES && allowed[device])) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(&k_paged_prompt<T, HD, MODS, TERMS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) {
