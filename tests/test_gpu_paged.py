@@ -871,3 +871,70 @@ def test_attention_in_place(ctx, dtype, dim, lens, news):
     packed[:, 1:1 + h] = q
     got = ctx.wisv_paged_attention(packed[:, 1:1 + h], *args, out=packed[:, 1:1 + h])
     assert torch.equal(got, want) and (packed[:, 0] == 7).all() and (packed[:, 1 + h:] == 7).all()
+
+
+@pytest.mark.parametrize("dim,g,lens,news", [(128, 8, [500, 300], [5, 7]), (128, 8, [700], [300]), (64, 8, [1500], [200]), (256, 4, [300, 90], [60, 90])])
+def test_prompts_offsets_beyond_32_bits(ctx, dim, g, lens, news):
+    """Pools of more than 2^31 elements whose last pages hold the requests, on the kernel of many rows (both its forms at head_dim 128)."""
+    page, h = 64, 4 * g
+    n_pages = 2 ** 31 // (g * page * dim) + 40
+    kp, vp = (torch.zeros((n_pages,) + s, dtype=BF16, device=DEV) for s in ((g, page, dim), (g, page // 8, dim, 8)))
+    q, ks, vs, small, starts = setup(BF16, dim, h, g, page, lens, news)
+    m = ks.shape[0]
+    kp[n_pages - m:], vp[n_pages - m:] = ks, vs
+    far = np.where(small >= 0, small + n_pages - m, -1)
+    args = (ints(starts), ints(lens), max(news), max(lens))
+    near = ctx.wisv_paged_attention(q, ks, vs, ints(small), *args)
+    assert near.any() and torch.equal(near, ctx.wisv_paged_attention(q, kp, vp, ints(far), *args))
+
+
+def test_float_prompts_offsets_beyond_32_bits(ctx):
+    page, h, g, dim, lens, news = 64, 32, 16, 128, [290, 260, 512, 256], [256, 256, 230, 256]
+    n_pages = 2 ** 31 // (g * page * dim) + 40
+    kp, vp = (torch.zeros((n_pages,) + s, dtype=F32, device=DEV) for s in ((g, page, dim), (g, page // 8, dim, 8)))
+    q, ks, vs, small, starts = setup(F32, dim, h, g, page, lens, news)
+    m = ks.shape[0]
+    kp[n_pages - m:], vp[n_pages - m:] = ks, vs
+    far = np.where(small >= 0, small + n_pages - m, -1)
+    args = (ints(starts), ints(lens), max(news), max(lens))
+    near = ctx.wisv_paged_attention(q, ks, vs, ints(small), *args)
+    assert near.any() and torch.equal(near, ctx.wisv_paged_attention(q, kp, vp, ints(far), *args))
+
+
+CAPTURED_FIRST = '''
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import torch
+import test_gpu_paged as t
+ctx = t.binding.Context(t.configs.get(0).model, t.gen.make_weights(t.configs.get(0).model, 0, t.DEV), 1, 32, 1)
+calls = []
+for dtype, dim, h, g, lens, news in {cases!r}:
+    q, kp, vp, table, starts = t.setup(getattr(torch, dtype), dim, h, g, 16, lens, news)
+    args = (q, kp, vp, t.ints(table), t.ints(starts), t.ints(lens), max(news), max(lens))
+    calls.append((args, torch.zeros_like(q)))
+torch.cuda.synchronize()
+for args, out in calls:
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.wisv_paged_attention(*args, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert out.any() and torch.equal(out, ctx.wisv_paged_attention(*args))
+        torch.cuda.synchronize()
+    print("captured", args[0].shape, flush=True)
+print("done", flush=True)
+'''
+
+
+def test_the_first_paged_call_of_a_process_may_be_captured():
+    """In a process of its own: the first call of each kernel of prompts, which asks for its LDS then, is the captured one."""
+    import os
+    import subprocess
+    import sys
+    tests = os.path.dirname(os.path.abspath(__file__))
+    cases = [("bfloat16", 128, 8, 2, [300, 200], [90, 60]), ("bfloat16", 128, 8, 2, [300, 200], [8, 5]), ("bfloat16", 256, 4, 2, [170], [60]),
+             ("bfloat16", 64, 8, 2, [9000], [60]), ("float32", 128, 32, 16, [290, 260, 512, 256], [256, 256, 230, 256])]
+    code = CAPTURED_FIRST.format(root=os.path.dirname(tests), tests=tests, cases=cases)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.strip().endswith("done"), r.stdout + r.stderr
