@@ -275,6 +275,9 @@ int wisv_ss_decide_static(wisv_ctx *ctx, int32_t batch, int32_t k, int32_t vocab
  *   n_used    [1] entries of free_pages that were dealt
  *   status    [batch] 0, or why the request is refused (its table row stays as it was): bits 1 free_pages is exhausted,
  *             2 the table's row is too short, 4 its rows end behind max_tokens
+ * A refused request keeps its rows in q_start; nothing is stored for them, and an attention of the step gives them outputs that mean
+ * nothing (of positions that end at cached_len): status says which to leave out.  One that is refused for pages uses up its turn: those
+ * behind it that need pages are refused as well, those that need none are served.
  * cached_len and new_len may lie in memory that the call writes: kv_len may be cached_len, so that a step's plan takes up the
  * last one's (one workgroup then does the work).  Otherwise no output may overlap another, free_pages or block_table. */
 #define WISV_PAGED_NO_PAGES 1
@@ -320,17 +323,19 @@ int wisv_paged_append(wisv_ctx *ctx, const wisv_paged_append_args *args);
  * rows of request b has position p = kv_len[b] - n + i and sees key j if j < kv_len[b] and
  *     j < prefix_len[b],  or  j <= p and (window == 0 or j > p - window).
  * Its score is x = scale * q.k, then softcap * tanh(x / softcap) if softcap > 0, then x + slopes[head] * (j - p) if slopes
- * are given; the output is the softmax-weighted sum of the values, and 0 for a row that sees no key (or none with a score
- * above minus infinity).  Query head h reads KV
- * head h / (n_heads / n_kv_heads).
+ * are given (signed: keys ahead of the row, which a prefix shows, gain by a positive slope); the output is the softmax-weighted
+ * sum of the values, and 0 for a row that sees no key (or none with a score above minus infinity).  Query head h reads KV head
+ * h / (n_heads / n_kv_heads).
  * Keys and values that a row does not see do not reach its output, whatever they hold; a value that it sees and that is
  * not finite makes that feature of its output infinite or NaN.  Rows of q behind q_start[batch] are
  * neither read nor written, nor are those before q_start[0].  kv_len beyond max_pages * page_size leaves the positions behind the table unseen.
  * out may be q (with the same stride); otherwise what the call writes, the workspace included, overlaps nothing that it reads.
- * max_new and max_len say how many new rows and how long a request is at most (0: unknown).  They choose how the work is
- * cut; requests beyond them are served all the same, more slowly.
+ * max_new and max_len say how many new rows and how long a request is at most (0: unknown, counted as n_tokens and the table's
+ * width).  They choose how the work is cut; requests beyond them are served all the same, more slowly; many single tokens
+ * without max_new run on tiles of 128 rows.  With a window the cut counts its positions and not a prefix's in front of it.
  * Arithmetic: scores, softmax and sums in float; WISV_BF16 rounds once at the end, and probabilities enter the matrix cores as
- * two bf16 terms (to 2^-17) where max_new * n_heads / n_kv_heads is at most 32, else as one (to 2^-8) or two.  Equal calls give equal bits.
+ * two bf16 terms (to 2^-17) where max_new * n_heads / n_kv_heads is at most 32, else as one (to 2^-8) or two; a capped
+ * score is off by up to 2^-21 of the cap.  Equal calls give equal bits.
  * workspace: at least what wisv_paged_attention_workspace says for the same arguments (it reads no pointer but notes which are NULL);
  * nothing in it has to be cleared or kept between calls.  Calls that may overlap, and graphs that may be replayed together,
  * need one each. */

@@ -469,7 +469,8 @@ class Context:
     def wisv_paged_plan(self, cached_len: torch.Tensor, new_len: torch.Tensor, free_pages: torch.Tensor,
                         block_table: torch.Tensor, page_size: int, max_tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
         """Plans a step: cached_len, new_len int32 [batch], free_pages int32 [n_free], block_table int32 [batch, max_pages]
-        (updated in place).  `out`: the tensors of an earlier plan of the same sizes, to be written again; cached_len may be its kv_len."""
+        (updated in place).  Requests with a status other than 0 are refused: what the step computes for their rows means nothing.
+        `out`: the tensors of an earlier plan of the same sizes, to be written again; cached_len may be its kv_len."""
         b, n_free = cached_len.numel(), free_pages.numel()
         if block_table.dim() != 2:
             raise ValueError("block_table must be [batch, max_pages]")
@@ -549,7 +550,8 @@ class Context:
                              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the rows q [tokens, heads, head_dim] over the pages, without a gradient; q_start int32 [batch + 1], kv_len int32 [batch],
         block_table int32 [batch, max_pages], slopes float32 [heads], prefix_len int32 [batch].  max_new, max_len: how many
-        new rows and how many positions a request has at most (0: unknown).  A new `out` is made where none is given (it may be q with
+        new rows and how many positions a request has at most (0: unknown; batches of few rows are slower without max_new, and bfloat16
+        ones less exact).  A new `out` is made where none is given (it may be q with
         its strides): rows behind q_start[batch] are left as they are in either.  workspace: a tensor of at least as many bytes as
         wisv_paged_attention_workspace asks for, kept by a caller whose calls must not allocate."""
         n, g, ps, hd, dtype, stride = self._pools(k_pages, v_pages)

@@ -446,16 +446,18 @@ PagedCut paged_cut(const PagedAttn &a, bool bf16, int head_dim, int max_new, int
     // 64, 338 and 514; head_dim 32: 30 of 500 behind 500, 8 / 2, 157 and 167
     const int64_t all_rows = (int64_t)a.n_tokens * a.rep, tiles_each = (all_rows + 128 * (int64_t)a.batch - 1) / (128 * (int64_t)a.batch);
     c.prompt = many && (bf16 || (head_dim >= 64 && all_rows / 128 * a.G >= 128 && all_rows >= 96 * tiles_each * a.batch));
-    // positions that a tile's rows see at most: a window's are those of its first row and what its rows span
+    // positions that a tile's rows see at most: a window's are those of its first row and what its rows span.  (A prefix in front of the
+    // window is not counted, and the last split has all that is left: one token over 12000 positions, 32 / 8 heads of 128, without a window
+    // 16.5 us, with one of 512 11, and with a prefix of 8000 80.)
     const int reach = a.window ? (int)std::min<int64_t>(max_len, (int64_t)a.window + 64 + (c.prompt ? 128 / a.rep : max_new)) : max_len;
     const int64_t steps = (reach + 63) / 64;
     if (c.prompt) {
         // Splitting the keys fills a chip, or the last of its rounds, that is not full.  In steps of 64 keys, in bf16 about 2 us each: a
         // split costs six (its start, its way to the join), the join three and the parts' way through memory; float steps are as much
         // longer as its products.  us per call: six prompts of up to 777 behind 900, 28 / 4 heads of 64, with a bias 1 split 43, 2 36.7, 3
-        // 36.0, 4 36.2, the rule's 35.0; one of 723 behind 20990, 56 / 8 of 64, with a cap 548, 490, 437, 420, the rule's 481; two of 2048
-        // behind 6144, 32 / 8 of 128, 1 (taken) 482, 2 537; float, one of 2048 behind 20000, 8 / 2 of 128, with a cap 3417, 2636, 1993,
-        // 4 (taken) 1518, 6 1567
+        // 36.0, 4 36.2, the rule's 35.0; one of 723 behind 20990, 56 / 8 of 64, with a cap 1 split 548, 2 (taken) 490, 3 437, 4 420: there
+        // the charge for rounds that are not whole is too high; two of 2048 behind 6144, 32 / 8 of 128, 1 (taken) 482, 2 537; float, one of
+        // 2048 behind 20000, 8 / 2 of 128, with a cap 3417, 2636, 1993, 4 (taken) 1518, 6 1567
         const double wgs = (double)std::max<int64_t>(((int64_t)a.n_tokens * a.rep + 127) / 128, a.batch) * a.G, slots = 256 * paged_prompt_wgs(bf16, head_dim);
         const double fixed = bf16 ? 1 : 18.0 / head_dim;
         const double part = (double)a.n_tokens * a.H * head_dim * 8 / 9e6;

@@ -1177,7 +1177,8 @@ static int paged_attention_args(Ctx *c, const wisv_paged_attention_args *args, P
     if (p.max_pages < 1 || (int64_t)p.max_pages * p.page_size > 1 << 30)
         return fail(c, WISV_EINVAL, "wisv_paged_attention: max_pages must be positive and max_pages * page_size at most 2^30");
     if (p.max_new < 0 || p.max_len < 0 || p.window < 0) return fail(c, WISV_EINVAL, "wisv_paged_attention: max_new, max_len or window is negative");
-    // (bf16 calls have a cap's tanh to 2^-23 of the cap: up to 2^14 that is within a probability's own rounding)
+    // (bf16 calls have a cap's tanh as 1 - 2 / (e + 1), to 2^-21: exponential, sum, reciprocal and result round.  Times the cap that is a
+    // score's, and a probability's relative, error: up to 2^4 below what two bf16 terms lose, up to 2^13 below one, at 2^14 twice that)
     if ((p.softcap != 0.f && !(p.softcap >= 1e-30f && p.softcap <= 16384.f)) || !isfinite(p.scale))
         return fail(c, WISV_EINVAL, "wisv_paged_attention: softcap must be 0 or from 1e-30 to 16384, scale finite");
     // (the kernels hold 2 scale / ln 2, divided by a cap: infinite, it would make a score of 0 no number)
