@@ -9,7 +9,7 @@ namespace wisv {
 // ------------------------------------------------------------------------------------------ step planning
 // One launch: every workgroup scans the lengths for itself (two prefix sums over the requests, kept in LDS) and then
 // writes its share of the table and of the tokens; no workgroup waits for another.  Bound by the latency of launch,
-// loads and scan: 5.5 us for 16 requests of 6 tokens, 6.2 for 512 with 22171 (a launch that does nothing takes 2.3).
+// loads and scan: 5.2 us for 16 requests of 6 tokens, 5.9 for 512 with 22171 (a launch that does nothing takes 2.3).
 // A workgroup reads the lengths once, before it writes anything, so that one alone may write over them (in a graph, the 512
 // requests 11.7 us instead of 5.5).
 constexpr int PLAN_THREADS = 256, PLAN_THREADS_ALONE = 1024;
